@@ -56,6 +56,9 @@ enum { QSVD_CACHE_F16 = 0, QSVD_CACHE_I8 = 1, QSVD_CACHE_I4 = 2 };
  * attention; AUTO picks the faster one for the layer (ABSORBED). */
 enum { QSVD_ATTN_AUTO = 0, QSVD_ATTN_ABSORBED = 1, QSVD_ATTN_RECONSTRUCT = 2 };
 
+/* 16-bit element types of the layer operators. */
+enum { QSVD_F16 = 0, QSVD_BF16 = 1 };
+
 /* Which up-projection outputs qsvd_lowrank_qkv_prefill writes. */
 enum { QSVD_OUT_Q = 1, QSVD_OUT_K = 2, QSVD_OUT_V = 4 };
 
@@ -324,6 +327,74 @@ qsvd_status qsvd_latent_decode_attention_rope(const qsvd_layer* w, const qsvd_ca
 
 size_t qsvd_decode_workspace_size(const qsvd_layer* w, const qsvd_cache* c, int32_t q_len,
                                   int32_t mode);
+
+/* ---- The rest of a decoder layer around the attention path ----
+ * The layer's norms, its output projection and its gated MLP, on the same
+ * per-token activation codes and per-channel weight codes (Section 4 setup):
+ * a norm feeds qsvd_lowrank_qkv_prefill (codes), qsvd_decode_project_append
+ * (fp16 rows) or a linear layer; a linear layer adds its result to the
+ * residual stream that the next norm reads.  `dtype` (QSVD_F16 or QSVD_BF16)
+ * is the type of every 16-bit operand of a call.  None takes a workspace. */
+
+/* Residual addition, root-mean-square norm and per-token quantization of M rows:
+ *   h  = x + residual in fp32, rounded to dtype (h = x without a residual)
+ *   r  = fp32(1 / sqrt(mean_k h[k]^2 + eps)), the mean and the root in fp64
+ *   y  = (h * r) * gamma in fp32, each product rounded on its own
+ *   xq, sx = the quantizer of qsvd_quantize_act on the fp32 y (bits, clip)
+ *   x         device [M][ldx]
+ *   residual  device [M][ldr] or NULL
+ *   gamma     device [K]
+ *   h         device [M][ldh] or NULL (not stored); may be x or residual itself
+ *             (same address and stride)
+ *   y         device [M][ldy], rounded to dtype, or NULL
+ *   xq        device int8 [M][K] or packed int4 [M][K/2], and sx device fp32
+ *             [M], or both NULL; y or xq must be given
+ * Apart from h as stated, outputs do not overlap inputs or each other.
+ * A row whose a = clip * max |y| is below 2^-119 (Qm / a passes fp32) has scale
+ * 1 and codes 0, as an all-zero row has; a row with a y that is not finite (an
+ * infinity or NaN in x, a sum past dtype) has scale NaN and codes 0, and other
+ * rows are not affected.
+ * Requires K % 8 == 0, K <= 65536, M < 2^22, strides that are multiples of 8,
+ * 16-byte aligned x, residual, gamma, h and y, 8-byte aligned xq, eps > 0, bits 8
+ * or 4, 0 < clip <= 1. */
+qsvd_status qsvd_rmsnorm_quantize_act(const void* x, int64_t ldx, const void* residual, int64_t ldr,
+                                      const void* gamma, int64_t M, int32_t K, int32_t dtype, float eps,
+                                      int32_t bits, float clip, void* h, int64_t ldh, void* y, int64_t ldy,
+                                      void* xq, float* sx, void* stream);
+
+/* The gate of a gated MLP with per-token quantization of its M rows:
+ *   y = gate / (1 + exp(-gate)) * up in fp32, xq, sx = the quantizer on y
+ *   gate, up  device [M][ldg], [M][ldu]: the two halves of one product's rows
+ *             (up = gate + K elements, ldg = ldu = 2 K) or tensors of their own
+ *   xq        device int8 [M][K] or packed int4 [M][K/2]
+ *   sx        device fp32 [M]
+ * exp, the quotient and the product are evaluated in fp32 to a few units in the
+ * last place, so a code may differ by one from that of the exact y next to a
+ * rounding border.  Tiny rows, values that are not finite and requirements as
+ * for qsvd_rmsnorm_quantize_act. */
+qsvd_status qsvd_silu_mul_quantize_act(const void* gate, int64_t ldg, const void* up, int64_t ldu, int64_t M,
+                                       int32_t K, int32_t dtype, int32_t bits, float clip, void* xq, float* sx,
+                                       void* stream);
+
+/* W8A8 linear layer with a scale per token and per output channel:
+ *   y[m][n] = (f32(sum_k xq[m][k] wq[n][k]) * sx[m]) * sw[n] + bias[n] + residual[m][n]
+ * with an exact integer sum, every fp32 step rounded on its own (bias first,
+ * then residual, each only if given) and one rounding to dtype.
+ *   xq        device int8 [M][ldx], e.g. from qsvd_quantize_act with bits 8
+ *   sx        device fp32 [M]
+ *   wq        device int8 [N][K] (transposed: the contraction contiguous)
+ *   sw        device fp32 [N]
+ *   bias      device [N] or NULL
+ *   residual  device [M][ldr] or NULL
+ *   y         device [M][ldy]; may be residual itself (same address and stride),
+ *             and overlaps no other operand
+ * Requires K % 16 == 0, K <= 131072, ldx % 16 == 0, ldx <= 2^22, 16-byte aligned
+ * xq and wq, ceil(M / 128) * ceil(N / 128) < 2^24; any N >= 1 and row strides of residual and y (strides that
+ * are multiples of 8 on 16-byte aligned y, residual and bias move in 16-byte
+ * runs, others element by element with the same result). */
+qsvd_status qsvd_linear_i8(const void* xq, int64_t ldx, const float* sx, const void* wq, const float* sw,
+                           int64_t M, int32_t N, int32_t K, const void* bias, const void* residual,
+                           int64_t ldr, int32_t dtype, void* y, int64_t ldy, void* stream);
 
 const char* qsvd_status_string(qsvd_status s);
 const char* qsvd_last_error(void);

@@ -16,6 +16,7 @@ QSVD_OK, QSVD_ERR_INVALID_ARG, QSVD_ERR_UNSUPPORTED, QSVD_ERR_CAPACITY, QSVD_ERR
 QSVD_CACHE_F16, QSVD_CACHE_I8, QSVD_CACHE_I4 = 0, 1, 2
 QSVD_ATTN_AUTO, QSVD_ATTN_ABSORBED, QSVD_ATTN_RECONSTRUCT = 0, 1, 2
 QSVD_OUT_Q, QSVD_OUT_K, QSVD_OUT_V = 1, 2, 4
+QSVD_F16, QSVD_BF16 = 0, 1
 
 EXPORTED = [
     "qsvd_quantize_act", "qsvd_quantize_act_rotated", "qsvd_lowrank_qkv_prefill", "qsvd_prefill_workspace_size",
@@ -24,6 +25,7 @@ EXPORTED = [
     "qsvd_latent_decode_attention",
     "qsvd_latent_decode_attention_rope",
     "qsvd_decode_workspace_size", "qsvd_latent_decode_attention_noalloc", "qsvd_noalloc_scratch_bytes",
+    "qsvd_rmsnorm_quantize_act", "qsvd_silu_mul_quantize_act", "qsvd_linear_i8",
     "qsvd_status_string", "qsvd_last_error", "qsvd_profile_enable", "qsvd_profile_reset",
     "qsvd_profile_read",
 ]
@@ -79,6 +81,9 @@ def lib():
             "qsvd_decode_workspace_size": (SZ, [LP, CP, I32, I32]),
             "qsvd_latent_decode_attention_noalloc": (I32, [LP, CP, P, I32, I32, F, P, P]),
             "qsvd_noalloc_scratch_bytes": (SZ, []),
+            "qsvd_rmsnorm_quantize_act": (I32, [P, I64, P, I64, P, I64, I32, I32, F, I32, F, P, I64, P, I64, P, P, P]),
+            "qsvd_silu_mul_quantize_act": (I32, [P, I64, P, I64, I64, I32, I32, I32, F, P, P, P]),
+            "qsvd_linear_i8": (I32, [P, I64, P, P, P, I64, I32, I32, P, P, I64, I32, P, I64, P]),
             "qsvd_status_string": (ctypes.c_char_p, [I32]),
             "qsvd_last_error": (ctypes.c_char_p, []),
             "qsvd_profile_enable": (I32, [I32, ctypes.c_char_p]),
@@ -155,6 +160,20 @@ def qsvd_noalloc_scratch_bytes():
 
 def qsvd_decode_workspace_size(layer, cache, q_len, mode):
     return lib().qsvd_decode_workspace_size(ctypes.byref(layer), ctypes.byref(cache), q_len, mode)
+
+
+def qsvd_rmsnorm_quantize_act(x, ldx, residual, ldr, gamma, M, K, dtype, eps, bits, clip, h, ldh, y, ldy, xq, sx,
+                              stream):
+    return lib().qsvd_rmsnorm_quantize_act(x, ldx, residual, ldr, gamma, M, K, dtype, eps, bits, clip, h, ldh, y, ldy,
+                                           xq, sx, stream)
+
+
+def qsvd_silu_mul_quantize_act(gate, ldg, up, ldu, M, K, dtype, bits, clip, xq, sx, stream):
+    return lib().qsvd_silu_mul_quantize_act(gate, ldg, up, ldu, M, K, dtype, bits, clip, xq, sx, stream)
+
+
+def qsvd_linear_i8(xq, ldx, sx, wq, sw, M, N, K, bias, residual, ldr, dtype, y, ldy, stream):
+    return lib().qsvd_linear_i8(xq, ldx, sx, wq, sw, M, N, K, bias, residual, ldr, dtype, y, ldy, stream)
 
 
 def status_string(status):

@@ -547,6 +547,102 @@ qsvd_status qsvd_latent_decode_attention_rope(const qsvd_layer* w, const qsvd_ca
   return decode_attention(w, c, q, q_len, mode, sm_scale, rope_theta, out, ws, ws_bytes, stream);
 }
 
+// ---------------------------------------------------------------- layer operators
+// Longest row of the row operators: 16 waves with eight 8-element chunks per lane.
+constexpr int32_t kMaxRowK = 65536;
+// A launch has fewer than 2^32 threads: rows of up to 1024 threads each, and
+// tiles of 128 x 128 outputs (smaller ones are for few of them) of 256.
+constexpr int64_t kMaxRows = ((int64_t)1 << 22) - 1;
+constexpr int64_t kMaxTiles = ((int64_t)1 << 24) - 1;
+// Contraction of a W8A8 product whose sum of int8 products fits an int32:
+// 131072 * 128 * 127 < 2^31.
+constexpr int32_t kMaxLinearK = 131072;
+// Widest row stride of codes: a tile's 256 row offsets fit 31 bits.
+constexpr int64_t kMaxLinearLd = (int64_t)1 << 22;
+
+static qsvd_status check_dtype(int32_t dtype) {
+  if (dtype != QSVD_F16 && dtype != QSVD_BF16) return fail(QSVD_ERR_INVALID_ARG, "dtype must be QSVD_F16 or QSVD_BF16");
+  return QSVD_OK;
+}
+
+static qsvd_status check_rows(int64_t M, int32_t K, int32_t dtype, int32_t bits, float clip) {
+  if (M < 0 || K <= 0) return fail(QSVD_ERR_INVALID_ARG, "bad sizes M=%lld K=%d", (long long)M, K);
+  const qsvd_status st = check_dtype(dtype);
+  if (st != QSVD_OK) return st;
+  if (bits != 8 && bits != 4) return fail(QSVD_ERR_INVALID_ARG, "bits must be 8 or 4");
+  if (!(clip > 0.f && clip <= 1.f)) return fail(QSVD_ERR_INVALID_ARG, "clip must be in (0, 1]");
+  if (K % 8) return fail(QSVD_ERR_UNSUPPORTED, "K must be a multiple of 8");
+  if (K > kMaxRowK) return fail(QSVD_ERR_UNSUPPORTED, "K must be at most %d", kMaxRowK);
+  if (M > kMaxRows) return fail(QSVD_ERR_UNSUPPORTED, "M must be at most %lld", (long long)kMaxRows);
+  return QSVD_OK;
+}
+
+// A 16-bit row operand (p NULL: absent): stride at least K, rows of 16-byte runs.
+static qsvd_status check_row_operand(const char* name, const void* p, int64_t ld, int32_t K) {
+  if (!p) return QSVD_OK;
+  if (ld < K) return fail(QSVD_ERR_INVALID_ARG, "row stride of %s %lld < K %d", name, (long long)ld, K);
+  if (ld % 8 || !aligned(p, 16))
+    return fail(QSVD_ERR_UNSUPPORTED, "%s must be 16-byte aligned with a row stride that is a multiple of 8", name);
+  return QSVD_OK;
+}
+
+qsvd_status qsvd_rmsnorm_quantize_act(const void* x, int64_t ldx, const void* residual, int64_t ldr, const void* gamma,
+                                      int64_t M, int32_t K, int32_t dtype, float eps, int32_t bits, float clip,
+                                      void* h, int64_t ldh, void* y, int64_t ldy, void* xq, float* sx, void* stream) {
+  qsvd_status st = check_rows(M, K, dtype, bits, clip);
+  if (st != QSVD_OK) return st;
+  if (!(eps > 0.f) || isinf(eps)) return fail(QSVD_ERR_INVALID_ARG, "eps must be finite and > 0");
+  if (M == 0) return QSVD_OK;
+  if (!x || !gamma) return fail(QSVD_ERR_INVALID_ARG, "NULL x/gamma");
+  if (!y && !xq) return fail(QSVD_ERR_INVALID_ARG, "neither y nor xq is given");
+  if (!xq != !sx) return fail(QSVD_ERR_INVALID_ARG, "xq and sx are given together or not at all");
+  const struct { const char* name; const void* p; int64_t ld; } rows[] = {
+      {"x", x, ldx}, {"residual", residual, ldr}, {"h", h, ldh}, {"y", y, ldy}};
+  for (const auto& r : rows)
+    if ((st = check_row_operand(r.name, r.p, r.ld, K)) != QSVD_OK) return st;
+  if (!aligned(gamma, 16) || !aligned(xq, 8)) return fail(QSVD_ERR_UNSUPPORTED, "gamma must be 16-byte and xq 8-byte aligned");
+  const NormArgs a{x, ldx, residual, ldr, gamma, M, K, dtype, eps, bits, clip, h, ldh, y, ldy, xq, sx};
+  return hip_status(launch_rmsnorm_quantize(a, (hipStream_t)stream), "rmsnorm_quantize_act");
+}
+
+qsvd_status qsvd_silu_mul_quantize_act(const void* gate, int64_t ldg, const void* up, int64_t ldu, int64_t M, int32_t K,
+                                       int32_t dtype, int32_t bits, float clip, void* xq, float* sx, void* stream) {
+  qsvd_status st = check_rows(M, K, dtype, bits, clip);
+  if (st != QSVD_OK) return st;
+  if (M == 0) return QSVD_OK;
+  if (!gate || !up || !xq || !sx) return fail(QSVD_ERR_INVALID_ARG, "NULL pointer");
+  if ((st = check_row_operand("gate", gate, ldg, K)) != QSVD_OK) return st;
+  if ((st = check_row_operand("up", up, ldu, K)) != QSVD_OK) return st;
+  if (!aligned(xq, 8)) return fail(QSVD_ERR_UNSUPPORTED, "xq must be 8-byte aligned");
+  const GateArgs a{gate, ldg, up, ldu, M, K, dtype, bits, clip, xq, sx};
+  return hip_status(launch_silu_mul_quantize(a, (hipStream_t)stream), "silu_mul_quantize_act");
+}
+
+qsvd_status qsvd_linear_i8(const void* xq, int64_t ldx, const float* sx, const void* wq, const float* sw, int64_t M,
+                           int32_t N, int32_t K, const void* bias, const void* residual, int64_t ldr, int32_t dtype,
+                           void* y, int64_t ldy, void* stream) {
+  if (M < 0 || N <= 0 || K <= 0) return fail(QSVD_ERR_INVALID_ARG, "bad sizes M=%lld N=%d K=%d", (long long)M, N, K);
+  qsvd_status st = check_dtype(dtype);
+  if (st != QSVD_OK) return st;
+  if (ldx < K) return fail(QSVD_ERR_INVALID_ARG, "row stride of xq %lld < K %d", (long long)ldx, K);
+  if (ldy < N) return fail(QSVD_ERR_INVALID_ARG, "row stride of y %lld < N %d", (long long)ldy, N);
+  if (residual && ldr < N) return fail(QSVD_ERR_INVALID_ARG, "row stride of residual %lld < N %d", (long long)ldr, N);
+  if (M == 0) return QSVD_OK;
+  if (!xq || !sx || !wq || !sw || !y) return fail(QSVD_ERR_INVALID_ARG, "NULL pointer");
+  if (K % 16 || ldx % 16) return fail(QSVD_ERR_UNSUPPORTED, "K and the row stride of xq must be multiples of 16");
+  if (K > kMaxLinearK) return fail(QSVD_ERR_UNSUPPORTED, "K must be at most %d", kMaxLinearK);
+  if (ldx > kMaxLinearLd) return fail(QSVD_ERR_UNSUPPORTED, "the row stride of xq must be at most %lld", (long long)kMaxLinearLd);
+  if (!aligned(xq, 16) || !aligned(wq, 16)) return fail(QSVD_ERR_UNSUPPORTED, "xq and wq must be 16-byte aligned");
+  if (!aligned(y, 2) || !aligned(residual, 2) || !aligned(bias, 2))
+    return fail(QSVD_ERR_UNSUPPORTED, "y, residual and bias must be aligned to their elements");
+  if ((M + 127) / 128 > kMaxTiles / (((int64_t)N + 127) / 128))
+    return fail(QSVD_ERR_UNSUPPORTED, "ceil(M / 128) * ceil(N / 128) must be at most %lld", (long long)kMaxTiles);
+  const bool vec = ldy % 8 == 0 && aligned(y, 16) && (!residual || (ldr % 8 == 0 && aligned(residual, 16))) &&
+                   aligned(bias, 16);
+  const LinearArgs p{(const int8_t*)xq, ldx, sx, (const int8_t*)wq, sw, M, N, K, bias, residual, ldr, dtype, y, ldy, vec};
+  return hip_status(launch_linear_i8(p, (hipStream_t)stream), "linear_i8");
+}
+
 qsvd_status qsvd_profile_enable(int32_t on, const char* filter) {
   std::lock_guard<std::mutex> lk(g_prof_mu);
   g_prof_on = on != 0;

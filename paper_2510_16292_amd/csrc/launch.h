@@ -176,4 +176,58 @@ struct CacheAttnArgs {
 };
 hipError_t launch_cache_attention(const CacheAttnArgs& c, hipStream_t s);
 
+// Row operators with the per-token quantizer fused in (dtype: QSVD_F16 / QSVD_BF16
+// of every 16-bit operand; strides in elements).
+struct NormArgs {
+  const void* x;
+  int64_t ldx;
+  const void* residual;     // NULL: none
+  int64_t ldr;
+  const void* gamma;
+  int64_t M;
+  int32_t K, dtype;
+  float eps;
+  int32_t bits;
+  float clip;
+  void* h;                  // x + residual, NULL: not stored
+  int64_t ldh;
+  void* y;                  // the normed rows, NULL: not stored
+  int64_t ldy;
+  void* xq;                 // their codes and scales, NULL: none
+  float* sx;
+};
+hipError_t launch_rmsnorm_quantize(const NormArgs& a, hipStream_t s);
+
+struct GateArgs {
+  const void* gate;
+  int64_t ldg;
+  const void* up;
+  int64_t ldu;
+  int64_t M;
+  int32_t K, dtype, bits;
+  float clip;
+  void* xq;
+  float* sx;
+};
+hipError_t launch_silu_mul_quantize(const GateArgs& a, hipStream_t s);
+
+// W8A8 linear layer: y = 16-bit((f32(x w^T) * sx[m]) * sw[n] + bias[n] + residual[m][n]).
+struct LinearArgs {
+  const int8_t* x;          // [M][ldx]
+  int64_t ldx;
+  const float* sx;
+  const int8_t* w;          // [N][K]
+  const float* sw;
+  int64_t M;
+  int32_t N, K;
+  const void* bias;         // NULL: none
+  const void* residual;     // NULL: none
+  int64_t ldr;
+  int32_t dtype;
+  void* y;
+  int64_t ldy;
+  bool vec;                 // bias, residual and y move in 16-byte runs
+};
+hipError_t launch_linear_i8(const LinearArgs& p, hipStream_t s);
+
 }  // namespace qsvd

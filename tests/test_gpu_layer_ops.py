@@ -1,0 +1,483 @@
+"""The layer operators (norm, gate, W8A8 linear) through the C ABI against their
+plain definitions (oracle/layer_oracle.py), alone and chained as a decoder
+layer uses them."""
+import numpy as np
+import pytest
+
+import gpu_harness as H
+from oracle import layer_oracle as L
+from paper_2510_16292_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+F16, BF16 = B.QSVD_F16, B.QSVD_BF16
+GUARD = 8                 # elements written around every output, which must stay
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    import torch
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    B.lib()
+
+
+def tdtype(dt):
+    t = H.torch()
+    return t.bfloat16 if dt == BF16 else t.float16
+
+
+def up16(a, dt, ld=None):
+    """fp32-held 16-bit rows on the device, row stride ld (the rest of a row NaN)."""
+    t = H.torch()
+    a = np.ascontiguousarray(a, dtype=np.float32)
+    if ld is None:
+        return t.from_numpy(a).cuda().to(tdtype(dt))
+    full = np.full((a.shape[0], ld), np.nan, np.float32)
+    full[:, :a.shape[1]] = a
+    return t.from_numpy(full).cuda().to(tdtype(dt))
+
+
+def down16(t_):
+    H.torch().cuda.synchronize()
+    return t_.float().cpu().numpy()
+
+
+class Guarded:
+    """A [rows][ld] output whose unused columns and a row behind the last hold a
+    pattern that must stay."""
+
+    def __init__(self, rows, cols, ld, dtype, offset=0):
+        t = H.torch()
+        self.rows, self.cols, self.ld = rows, cols, ld
+        self.flat = t.full((offset + (rows + 1) * ld + GUARD,), 77, dtype=dtype, device="cuda")
+        self.view = self.flat[offset:offset + (rows + 1) * ld].view(rows + 1, ld)
+        self.offset = offset
+
+    @property
+    def ptr(self):
+        return self.view.data_ptr()
+
+    def get(self):
+        H.torch().cuda.synchronize()
+        v = self.view.float().cpu().numpy()
+        assert (v[self.rows] == 77).all() and (v[:self.rows, self.cols:] == 77).all(), "written outside the output"
+        assert (self.flat[:self.offset].float().cpu().numpy() == 77).all()
+        return v[:self.rows, :self.cols]
+
+
+def unpack(codes, bits, K):
+    codes = codes.astype(np.int64).astype(np.int8)
+    if bits == 8:
+        return codes
+    lo, hi = (codes << 4).astype(np.int8) >> 4, codes >> 4
+    return np.stack([lo, hi], axis=-1).reshape(codes.shape[0], K)
+
+
+def rows16(g, M, K, bf16, scale=1.0):
+    x = g.standard_normal((M, K)) * scale * np.exp(0.7 * g.standard_normal((M, 1)))
+    x[:, g.integers(0, K, max(1, K // 100))] *= 30
+    return L.round16(x, bf16)
+
+
+# ---------------------------------------------------------------- norm
+
+def run_norm(x, res, gamma, dt, bits=8, clip=1.0, eps=1e-6, want=("h", "y", "q"), pad=0, alias=None, stream=None):
+    t = H.torch()
+    M, K = x.shape
+    ld = K + pad
+    xd, gd = up16(x, dt, ld), up16(gamma[None], dt)
+    rd = None if res is None else up16(res, dt, ld + (8 if pad else 0))
+    hb = Guarded(M, K, ld, tdtype(dt)) if "h" in want and alias is None else None
+    h_ptr, h_ld = (hb.ptr, ld) if hb else (0, 0)
+    if alias is not None:
+        src = xd if alias == "x" else rd
+        h_ptr, h_ld = src.data_ptr(), src.shape[1]
+    yb = Guarded(M, K, ld, tdtype(dt)) if "y" in want else None
+    width = K * bits // 8
+    qb = Guarded(M, width, width, t.int8) if "q" in want else None
+    sb = Guarded(M, 1, 1, t.float32) if "q" in want else None
+    B.check(B.qsvd_rmsnorm_quantize_act(
+        xd.data_ptr(), ld, B.ptr(rd), 0 if rd is None else rd.shape[1], gd.data_ptr(), M, K, dt, eps, bits, clip,
+        h_ptr, h_ld, yb.ptr if yb else 0, ld if yb else 0, qb.ptr if qb else 0, sb.ptr if sb else 0,
+        stream or B.stream_handle()))
+    t.cuda.synchronize()
+    out = {}
+    if hb:
+        out["h"] = hb.get()
+    if alias is not None:
+        out["h"] = down16(xd if alias == "x" else rd)[:, :K]
+    if yb:
+        out["y"] = yb.get()
+    if qb:
+        out["q"], out["s"] = unpack(qb.get(), bits, K), sb.get()[:, 0]
+    return out
+
+
+def check_norm(got, x, res, gamma, dt, bits=8, clip=1.0, eps=1e-6):
+    """Bit for bit: the sum of squares in fp64 leaves fp32 steps that the
+    definition fixes."""
+    h, y, q, s = L.rmsnorm_quantize(x, res, gamma, eps, bits, clip, dt == BF16)
+    if "h" in got:
+        assert np.array_equal(got["h"], h, equal_nan=True)
+    if "y" in got:
+        assert np.array_equal(got["y"], L.round16(y, dt == BF16), equal_nan=True)
+    if "q" in got:
+        assert np.array_equal(got["s"], s, equal_nan=True)
+        assert np.array_equal(got["q"], q)
+
+
+@pytest.mark.parametrize("dt", [F16, BF16], ids=["f16", "bf16"])
+@pytest.mark.parametrize("M,K", [(1, 8), (3, 72), (2, 504), (130, 512), (5, 520), (16, 4096), (33, 4104), (300, 3584),
+                                 (1000, 1032), (7, 16392), (2, 32776), (2, 65536)])
+def test_norm_matches_definition(M, K, dt):
+    g = np.random.default_rng(M * 100003 + K)
+    bf = dt == BF16
+    x, res = rows16(g, M, K, bf), rows16(g, M, K, bf, 3.0)
+    gamma = L.round16(1 + 0.3 * g.standard_normal(K), bf)
+    for r in (res, None):
+        check_norm(run_norm(x, r, gamma, dt), x, r, gamma, dt)
+    check_norm(run_norm(x, res, gamma, dt, bits=4, clip=0.9, pad=24), x, res, gamma, dt, bits=4, clip=0.9)
+
+
+@pytest.mark.parametrize("want", [("y",), ("q",), ("h", "y"), ("h", "q"), ("y", "q")])
+def test_norm_output_choices(want):
+    g = np.random.default_rng(3)
+    x, res, gamma = rows16(g, 20, 1000, False), rows16(g, 20, 1000, False), L.round16(g.standard_normal(1000), False)
+    got = run_norm(x, res, gamma, F16, want=want)
+    assert ("h" in got, "y" in got, "q" in got) == ("h" in want, "y" in want, "q" in want)
+    check_norm(got, x, res, gamma, F16)
+
+
+@pytest.mark.parametrize("alias", ["x", "residual"])
+@pytest.mark.parametrize("M,K", [(3, 520), (40, 16392)])
+def test_norm_sum_in_place(M, K, alias):
+    g = np.random.default_rng(4)
+    x, res, gamma = rows16(g, M, K, False), rows16(g, M, K, False), L.round16(g.standard_normal(K), False)
+    check_norm(run_norm(x, res, gamma, F16, alias=alias), x, res, gamma, F16)
+
+
+@pytest.mark.parametrize("dt", [F16, BF16], ids=["f16", "bf16"])
+def test_norm_special_rows(dt):
+    """Zero rows, zero gamma columns, a tiny row, sums past the type, infinities
+    and NaN: only their own rows show it."""
+    bf = dt == BF16
+    K = 264
+    g = np.random.default_rng(5)
+    x = rows16(g, 9, K, bf)
+    res = np.zeros_like(x)
+    x[1] = 0
+    x[2] = L.round16(np.full(K, 2.0 ** -24), bf)
+    x[3, 7] = np.inf
+    x[4, 9] = np.nan
+    big = L.round16(np.float32(3e38 if bf else 65504), bf)
+    x[5, 3], res[5, 3] = big, big
+    x[6] = L.round16(np.full(K, 1e18 if bf else 6e4), bf)
+    x[7, :] = 0
+    x[7, K - 1] = 1
+    gamma = L.round16(g.standard_normal(K), bf)
+    gamma[::5] = 0
+    got = run_norm(x, res, gamma, dt)
+    check_norm(got, x, res, gamma, dt)
+    assert np.isnan(got["s"][[3, 4, 5]]).all() and np.isfinite(got["s"][[0, 1, 2, 6, 7, 8]]).all()
+    assert got["s"][1] == 1 and not got["q"][1].any()
+    zero = run_norm(x[:1], None, np.zeros(K, np.float32), dt)
+    assert zero["s"][0] == 1 and not zero["q"].any()
+
+
+def test_norm_then_quantizer_of_the_library():
+    """The codes of y = 1-gamma rows without rounding loss equal qsvd_quantize_act
+    of the rows the norm writes: h of two magnitudes whose norm is exact in fp16."""
+    g = np.random.default_rng(6)
+    M, K = 17, 256
+    x = np.where(g.random((M, K)) < 0.5, -1.0, 1.0).astype(np.float32) * np.float32(0.5)
+    gamma = L.round16(g.standard_normal(K), False)
+    got = run_norm(x, None, gamma, F16, eps=1e-30)
+    xq, sx = H.quantize_act(got["y"].astype(np.float16))
+    assert np.array_equal(xq.view(np.int8), got["q"]) and np.array_equal(sx, got["s"])
+
+
+# ---------------------------------------------------------------- gate
+
+def run_gate(gate, up, dt, bits=8, clip=1.0, halves=True, pad=0):
+    t = H.torch()
+    M, K = gate.shape
+    if halves:
+        both = up16(np.concatenate([gate, up], axis=1), dt, 2 * K + pad)
+        gp, upp, ldg, ldu, keep = both.data_ptr(), both.data_ptr() + 2 * K, 2 * K + pad, 2 * K + pad, both
+    else:
+        gd, ud = up16(gate, dt, K + pad), up16(up, dt, K + 2 * pad)
+        gp, upp, ldg, ldu, keep = gd.data_ptr(), ud.data_ptr(), K + pad, K + 2 * pad, (gd, ud)
+    width = K * bits // 8
+    qb, sb = Guarded(M, width, width, t.int8), Guarded(M, 1, 1, t.float32)
+    B.check(B.qsvd_silu_mul_quantize_act(gp, ldg, upp, ldu, M, K, dt, bits, clip, qb.ptr, sb.ptr, B.stream_handle()))
+    t.cuda.synchronize()
+    del keep
+    return unpack(qb.get(), bits, K), sb.get()[:, 0]
+
+
+def check_gate(got, gate, up, bits=8, clip=1.0):
+    """Against the exact values.  y takes a hardware 2^p (1 ulp), its remainder's
+    factor (1.5), 1 + e (0.5), a hardware reciprocal (1) and two products (1) --
+    below 8 ulp in all, 2^-21 relative; the scale adds its own three roundings.
+    So a code is the exact one unless the exact y / step is within
+    127 * 2^-19 of a border between two codes, and then off by one at most."""
+    q, s = got
+    y = L.silu_mul(gate, up)
+    qm = 2.0 ** (bits - 1) - 1
+    a = clip * np.abs(y).max(axis=1)
+    step = np.where(a > 0, a / qm, 1.0)
+    assert np.all(np.abs(s - step) <= 2.0 ** -20 * step)
+    t = np.clip(y / step[:, None], -qm, qm)
+    near = np.abs(t - np.floor(t) - 0.5) <= 127 * 2.0 ** -19
+    d = np.abs(q.astype(np.float64) - np.rint(t))
+    assert d[~near].max(initial=0) == 0 and d.max(initial=0) <= 1
+    assert near.mean() < 0.01
+
+
+@pytest.mark.parametrize("dt", [F16, BF16], ids=["f16", "bf16"])
+@pytest.mark.parametrize("M,K", [(1, 8), (2, 136), (3, 704), (32, 2816), (300, 1000), (5, 9856), (3, 16392), (2, 40000),
+                                 (1, 65536)])
+def test_gate_matches_definition(M, K, dt):
+    g = np.random.default_rng(M * 7 + K)
+    gate = L.round16(3 * g.standard_normal((M, K)), dt == BF16)
+    up = L.round16(g.standard_normal((M, K)), dt == BF16)
+    check_gate(run_gate(gate, up, dt), gate, up)
+    check_gate(run_gate(gate, up, dt, bits=4, clip=0.9, halves=False, pad=16), gate, up, bits=4, clip=0.9)
+
+
+@pytest.mark.parametrize("dt", [F16, BF16], ids=["f16", "bf16"])
+def test_gate_special_rows(dt):
+    """Gates far to both sides, zero rows, infinities and NaN."""
+    bf = dt == BF16
+    K = 128
+    g = np.random.default_rng(8)
+    gate, up = (L.round16(g.standard_normal((10, K)), bf) for _ in range(2))
+    far = L.round16(np.float32(3e38 if bf else 65504), bf)
+    gate[1] = 0
+    up[2] = 0
+    gate[3] = -far                  # silu is 0
+    gate[4, :] = far / 4            # silu is the gate
+    up[4] = L.round16(g.uniform(0.5, 1, K), bf)
+    gate[5, 4] = np.nan
+    up[6, 5] = np.inf
+    gate[7] = L.round16(np.linspace(-30, 30, K), bf)
+    gate[8] = L.round16(np.linspace(-86, -80, K), bf)
+    gate[9] = L.round16(np.full(K, -150.0), bf)        # e^150 passes fp32: 0
+    q, s = run_gate(gate, up, dt)
+    fine = [0, 1, 2, 4, 7, 8]
+    check_gate((q[fine], s[fine]), gate[fine], up[fine])
+    for i in (1, 2, 3, 9):
+        assert s[i] == 1 and not q[i].any(), i
+    for i in (5, 6):
+        assert np.isnan(s[i]) and not q[i].any()
+
+
+# ---------------------------------------------------------------- linear
+
+def run_linear(xq, sx, wq, sw, dt, bias=None, res=None, ldx=None, ldy=None, offset=0, alias=False):
+    t = H.torch()
+    M, K = xq.shape
+    N = wq.shape[0]
+    ldx, ldy = ldx or K, ldy or N
+    xf = np.full((M, ldx), 113, np.int8)
+    xf[:, :K] = xq
+    xd, wd, sxd, swd = H.dev(xf), H.dev(wq), H.dev(sx.astype(np.float32)), H.dev(sw.astype(np.float32))
+    bd = None if bias is None else up16(bias[None], dt)
+    yb = Guarded(M, N, ldy, tdtype(dt), offset)
+    rd, ldr = None, 0
+    if res is not None and alias:
+        yb.view[:M, :N] = up16(res, dt)
+        r_ptr, ldr = yb.ptr, ldy
+    elif res is not None:
+        ldr = N + 3 if offset else N
+        rd = up16(res, dt, ldr)
+        r_ptr = rd.data_ptr()
+    else:
+        r_ptr = 0
+    B.check(B.qsvd_linear_i8(xd.data_ptr(), ldx, sxd.data_ptr(), wd.data_ptr(), swd.data_ptr(), M, N, K, B.ptr(bd),
+                             r_ptr, ldr, dt, yb.ptr, ldy, B.stream_handle()))
+    return yb.get()
+
+
+def linear_inputs(seed, M, N, K, bf16, full=False):
+    g = np.random.default_rng(seed)
+    if full:
+        xq, wq = (g.integers(-127, 128, (r, K)).astype(np.int8) for r in (M, N))
+    else:
+        xq = np.clip(np.rint(25 * g.standard_normal((M, K))), -127, 127).astype(np.int8)
+        wq = np.clip(np.rint(30 * g.standard_normal((N, K))), -127, 127).astype(np.int8)
+    sx = np.exp(g.uniform(-6, -2, M)).astype(np.float32)
+    sw = np.exp(g.uniform(-8, -5, N)).astype(np.float32)
+    bias, res = L.round16(g.standard_normal(N), bf16), L.round16(3 * g.standard_normal((M, N)), bf16)
+    return xq, sx, wq, sw, bias, res
+
+
+# Around the edges of every tile the product uses, short and odd contractions
+# (one 16-byte chunk, a partial stage of every length), one row to many.
+LINEAR = [(1, 1, 16), (1, 256, 256), (2, 17, 48), (5, 100, 112), (15, 1000, 1008), (16, 4096, 512), (17, 33, 144),
+          (31, 300, 2064), (32, 3584, 1264), (33, 257, 400), (48, 520, 3600), (63, 129, 128), (64, 1024, 4096),
+          (65, 64, 96), (100, 1001, 624), (127, 255, 80), (128, 128, 64), (129, 385, 1040), (200, 2000, 336),
+          (255, 24, 2048), (257, 513, 208), (333, 1001, 1008), (640, 1300, 528), (1000, 9, 4112), (2100, 2052, 160)]
+
+
+@pytest.mark.parametrize("dt", [F16, BF16], ids=["f16", "bf16"])
+@pytest.mark.parametrize("M,N,K", LINEAR)
+def test_linear_matches_definition(M, N, K, dt):
+    bf = dt == BF16
+    xq, sx, wq, sw, bias, res = linear_inputs(M + 7 * N + 11 * K, M, N, K, bf)
+    for b, r in ((None, None), (bias, res)):
+        got = run_linear(xq, sx, wq, sw, dt, b, r)
+        assert np.array_equal(got, L.linear_i8(xq, sx, wq, sw, b, r, bf))
+
+
+@pytest.mark.parametrize("M,N,K,ldx,ldy,offset", [
+    (3, 40, 64, 80, 48, 0), (20, 130, 272, 288, 131, 0), (40, 200, 272, 512, 208, 1), (150, 200, 144, 160, 201, 3),
+    (300, 136, 400, 416, 144, 8), (700, 600, 128, 144, 607, 5)])
+def test_linear_strides_and_alignment(M, N, K, ldx, ldy, offset):
+    xq, sx, wq, sw, bias, res = linear_inputs(M, M, N, K, False)
+    want = L.linear_i8(xq, sx, wq, sw, bias, res, False)
+    assert np.array_equal(run_linear(xq, sx, wq, sw, F16, bias, res, ldx, ldy, offset), want)
+    assert np.array_equal(run_linear(xq, sx, wq, sw, F16, bias, res, ldx, ldy, offset, alias=True), want)
+
+
+@pytest.mark.parametrize("M", [1, 32, 70, 300])
+def test_linear_longest_contraction(M):
+    """Every product 127 * 127 over the longest contraction: 131072 * 16129 is
+    below 2^31, partial sums as well."""
+    K, N = 131072, 40
+    xq = np.full((M, K), 127, np.int8)
+    wq = np.full((N, K), 127, np.int8)
+    wq[1::2] = -127
+    sx, sw = np.full(M, 2.0 ** -20, np.float32), np.full(N, 2.0 ** -4, np.float32)
+    acc = 127.0 * 127 * K * np.where(np.arange(N) % 2, -1, 1)
+    want = L.round16(np.broadcast_to(acc * 2.0 ** -24, (M, N)).astype(np.float32), True)
+    assert np.array_equal(run_linear(xq, sx, wq, sw, BF16), want)
+
+
+@pytest.mark.parametrize("M", [3, 40, 500])
+def test_linear_rows_that_are_not_finite_stay_alone(M):
+    xq, sx, wq, sw, bias, res = linear_inputs(2, M, 72, 160, False)
+    sx[1] = np.nan
+    res[2, 5] = np.inf
+    sx[0] = 1e30                                     # past fp16: infinities of the sum's sign
+    got = run_linear(xq, sx, wq, sw, F16, bias, res)
+    want = L.linear_i8(xq, sx, wq, sw, bias, res, False)
+    assert np.array_equal(got, want, equal_nan=True)
+    assert np.isnan(got[1]).all() and np.isinf(got[2, 5]) and np.isfinite(got[3:]).all()
+
+
+def test_linear_full_range_codes_many_tiles():
+    xq, sx, wq, sw, bias, res = linear_inputs(9, 1100, 2300, 1552, True, full=True)
+    got = run_linear(xq, sx, wq, sw, BF16, bias, res)
+    assert np.array_equal(got, L.linear_i8(xq, sx, wq, sw, bias, res, True))
+
+
+# ---------------------------------------------------------------- together
+
+class Mlp:
+    """x -> norm -> gate|up -> silu * up -> down + h, on the device."""
+
+    def __init__(self, M, d, f, dt, seed=0):
+        g = np.random.default_rng(seed)
+        self.M, self.d, self.f, self.dt = M, d, f, dt
+        bf = dt == BF16
+        self.gamma = L.round16(1 + 0.2 * g.standard_normal(d), bf)
+        self.w1, self.s1 = (np.clip(np.rint(30 * g.standard_normal((2 * f, d))), -127, 127).astype(np.int8),
+                            np.full(2 * f, 1 / (30 * np.sqrt(d)), np.float32))
+        self.w2, self.s2 = (np.clip(np.rint(30 * g.standard_normal((d, f))), -127, 127).astype(np.int8),
+                            np.full(d, 1 / (30 * np.sqrt(f)), np.float32))
+        self.dw = [H.dev(a) for a in (self.w1, self.s1, self.w2, self.s2)]
+        self.dg = up16(self.gamma[None], dt)
+        E, t = H.empty, H.torch()
+        self.x, self.res = E((M, d), tdtype(dt)), E((M, d), tdtype(dt))
+        self.h, self.y = E((M, d), tdtype(dt)), E((M, d), tdtype(dt))
+        self.gu = E((M, 2 * f), tdtype(dt))
+        self.q1, self.sx1 = E((M, d), t.int8), E((M,), t.float32)
+        self.q2, self.sx2 = E((M, f), t.int8), E((M,), t.float32)
+
+    def run(self, stream):
+        M, d, f, dt, P = self.M, self.d, self.f, self.dt, B.ptr
+        w1, s1, w2, s2 = self.dw
+        B.check(B.qsvd_rmsnorm_quantize_act(P(self.x), d, P(self.res), d, P(self.dg), M, d, dt, 1e-5, 8, 1.0, P(self.h),
+                                            d, 0, 0, P(self.q1), P(self.sx1), stream))
+        B.check(B.qsvd_linear_i8(P(self.q1), d, P(self.sx1), P(w1), P(s1), M, 2 * f, d, 0, 0, 0, dt, P(self.gu), 2 * f,
+                                 stream))
+        B.check(B.qsvd_silu_mul_quantize_act(P(self.gu), 2 * f, P(self.gu) + 2 * f, 2 * f, M, f, dt, 8, 1.0, P(self.q2),
+                                             P(self.sx2), stream))
+        B.check(B.qsvd_linear_i8(P(self.q2), f, P(self.sx2), P(w2), P(s2), M, d, f, 0, P(self.h), d, dt, P(self.y), d,
+                                 stream))
+
+    def load(self, x, res):
+        self.x.copy_(up16(x, self.dt))
+        self.res.copy_(up16(res, self.dt))
+
+    def outputs(self):
+        return [H.host(t.float()) for t in (self.h, self.q1, self.sx1, self.gu, self.q2, self.sx2, self.y)]
+
+
+@pytest.mark.parametrize("M,d,f,dt", [(1, 256, 704, F16), (16, 512, 1408, BF16), (70, 256, 704, BF16),
+                                      (333, 1024, 2816, F16)])
+def test_mlp_step_by_step(M, d, f, dt):
+    """Every operator of a chained MLP against its definition on what the one
+    before it wrote."""
+    bf = dt == BF16
+    g = np.random.default_rng(M)
+    x, res = rows16(g, M, d, bf), rows16(g, M, d, bf)
+    m = Mlp(M, d, f, dt)
+    m.load(x, res)
+    m.run(B.stream_handle())
+    h, q1, s1, gu, q2, s2, y = m.outputs()
+    ho, _, qo, so = L.rmsnorm_quantize(x, res, m.gamma, 1e-5, 8, 1.0, bf)
+    assert np.array_equal(h, ho) and np.array_equal(q1, qo) and np.array_equal(s1, so)
+    assert np.array_equal(gu, L.linear_i8(q1, s1, m.w1, m.s1, None, None, bf))
+    check_gate((q2.astype(np.int8), s2), gu[:, :f], gu[:, f:])
+    assert np.array_equal(y, L.linear_i8(q2, s2, m.w2, m.s2, None, h, bf))
+
+
+@pytest.mark.parametrize("M", [4, 200])
+def test_mlp_graph_replays_match_eager(M):
+    """Captured once, replayed with new inputs and eager work between: bit for
+    bit the eager result."""
+    t = H.torch()
+    d, f = 512, 1408
+    eager, graph = Mlp(M, d, f, F16), Mlp(M, d, f, F16)
+    g = np.random.default_rng(1)
+    graph.load(rows16(g, M, d, False), rows16(g, M, d, False))
+    side = t.cuda.Stream()
+    side.wait_stream(t.cuda.current_stream())
+    with t.cuda.stream(side):
+        graph.run(side.cuda_stream)
+    t.cuda.synchronize()
+    cg = t.cuda.CUDAGraph()
+    with t.cuda.graph(cg):
+        graph.run(B.stream_handle())
+    for _ in range(4):
+        x, res = rows16(g, M, d, False), rows16(g, M, d, False)
+        graph.load(x, res)
+        eager.load(x, res)
+        cg.replay()
+        eager.run(B.stream_handle())
+        t.cuda.synchronize()
+        for a, b in zip(graph.outputs(), eager.outputs()):
+            assert np.array_equal(a, b)
+
+
+def test_mlps_on_two_streams_at_once():
+    """No shared scratch: two layers in flight on two streams, each as alone."""
+    t = H.torch()
+    g = np.random.default_rng(2)
+    ms = [Mlp(64, 512, 1408, F16, seed=s) for s in (1, 2)]
+    want = []
+    for m in ms:
+        m.load(rows16(g, 64, 512, False), rows16(g, 64, 512, False))
+        m.run(B.stream_handle())
+        want.append(m.outputs())
+    streams = [t.cuda.Stream() for _ in ms]
+    t.cuda.synchronize()
+    for _ in range(5):
+        for m, s in zip(ms, streams):
+            m.run(s.cuda_stream)
+    t.cuda.synchronize()
+    for m, w in zip(ms, want):
+        for a, b in zip(m.outputs(), w):
+            assert np.array_equal(a, b)
