@@ -551,9 +551,9 @@ qsvd_status qsvd_latent_decode_attention_rope(const qsvd_layer* w, const qsvd_ca
 // Longest row of the row operators: 16 waves with eight 8-element chunks per lane.
 constexpr int32_t kMaxRowK = 65536;
 // A launch has fewer than 2^32 threads: rows of up to 1024 threads each, and
-// tiles of 128 x 128 outputs (smaller ones are for few of them) of 256.
+// tiles of at least 64 x 64 outputs of up to 512.
 constexpr int64_t kMaxRows = ((int64_t)1 << 22) - 1;
-constexpr int64_t kMaxTiles = ((int64_t)1 << 24) - 1;
+constexpr int64_t kMaxTiles = ((int64_t)1 << 23) - 1;
 // Contraction of a W8A8 product whose sum of int8 products fits an int32:
 // 131072 * 128 * 127 < 2^31.
 constexpr int32_t kMaxLinearK = 131072;
@@ -635,8 +635,8 @@ qsvd_status qsvd_linear_i8(const void* xq, int64_t ldx, const float* sx, const v
   if (!aligned(xq, 16) || !aligned(wq, 16)) return fail(QSVD_ERR_UNSUPPORTED, "xq and wq must be 16-byte aligned");
   if (!aligned(y, 2) || !aligned(residual, 2) || !aligned(bias, 2))
     return fail(QSVD_ERR_UNSUPPORTED, "y, residual and bias must be aligned to their elements");
-  if ((M + 127) / 128 > kMaxTiles / (((int64_t)N + 127) / 128))
-    return fail(QSVD_ERR_UNSUPPORTED, "ceil(M / 128) * ceil(N / 128) must be at most %lld", (long long)kMaxTiles);
+  if (M / 64 + 1 > kMaxTiles / (((int64_t)N + 63) / 64))
+    return fail(QSVD_ERR_UNSUPPORTED, "(M / 64 + 1) * ceil(N / 64) must be below 2^23");
   const bool vec = ldy % 8 == 0 && aligned(y, 16) && (!residual || (ldr % 8 == 0 && aligned(residual, 16))) &&
                    aligned(bias, 16);
   const LinearArgs p{(const int8_t*)xq, ldx, sx, (const int8_t*)wq, sw, M, N, K, bias, residual, ldr, dtype, y, ldy, vec};

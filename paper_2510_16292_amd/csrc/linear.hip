@@ -32,7 +32,48 @@ __device__ __forceinline__ void lin_wait_barrier() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
-template <int BM, int BN, int WM, int WN>
+// The same for a stage that `rem` stages (at most R count) were issued after.
+template <int LPW, int R>
+__device__ __forceinline__ void lin_wait_stage(int rem) {
+  if constexpr (R == 0) {
+    lin_wait_barrier<0>();
+  } else {
+    if (rem >= R) lin_wait_barrier<R * LPW>();
+    else lin_wait_stage<LPW, R - 1>(rem);
+  }
+}
+
+// Eight outputs of row m from column n (below N), scaled: bias and residual added,
+// rounded once and stored, in 16-byte runs where the operands allow it.
+template <bool BF>
+__device__ __forceinline__ void lin_store(const LinearArgs& p, int64_t m, int32_t n, float* v) {
+  using E = Elem16<BF>;
+  if (p.vec && n + 8 <= p.N) {
+    float b[8];
+    if (p.bias) {
+      E::unpack(*reinterpret_cast<const i32x4*>(reinterpret_cast<const uint16_t*>(p.bias) + n), b);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = add_rn(v[e], b[e]);
+    }
+    if (p.residual) {
+      E::unpack(*reinterpret_cast<const i32x4*>(reinterpret_cast<const uint16_t*>(p.residual) + m * p.ldr + n), b);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = add_rn(v[e], b[e]);
+    }
+    *reinterpret_cast<i32x4*>(reinterpret_cast<uint16_t*>(p.y) + m * p.ldy + n) = E::pack(v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if (n + e >= p.N) continue;
+      float o = v[e];
+      if (p.bias) o = add_rn(o, E::get(p.bias, n + e));
+      if (p.residual) o = add_rn(o, E::get(p.residual, m * p.ldr + n + e));
+      E::put(p.y, m * p.ldy + n + e, o);
+    }
+  }
+}
+
+template <int BM, int BN, int WM, int WN, int NS>
 struct LinCfg {
   static constexpr int kWaves = (BM / WM) * (BN / WN);
   static constexpr int kThreads = 64 * kWaves;
@@ -42,16 +83,18 @@ struct LinCfg {
   static constexpr int kStage = (kABlocks + kBBlocks) * 1024;
   static constexpr int kOutLd = WN + 4;                                   // staged fp32 row, 32 rows a wave
   static constexpr int kOut = kWaves * 32 * kOutLd * 4;
-  static constexpr size_t kLds = 2 * kStage > kOut ? 2 * kStage : kOut;
+  static constexpr size_t kLds = NS * kStage > kOut ? NS * kStage : kOut;
 };
 
-// BM x BN outputs per workgroup, two stages: one is multiplied while the next
-// one's direct loads (global memory straight into LDS) are in flight.
-template <bool BF, int BM, int BN, int WM, int WN>
-__global__ void __launch_bounds__((LinCfg<BM, BN, WM, WN>::kThreads))
+// BM x BN outputs per workgroup (WM x WN per wave), the contraction in stages of
+// 128 bytes, NS of them in LDS: NS - 1 stages' direct loads (global memory
+// straight into LDS) are in flight while one is multiplied; one barrier per
+// stage.  The fragments of a 32-byte step are read while the products of the
+// step before run.
+template <bool BF, int BM, int BN, int WM, int WN, int NS>
+__global__ void __launch_bounds__((LinCfg<BM, BN, WM, WN, NS>::kThreads))
 linear_tile_kernel(LinearArgs p, int32_t tiles_n, int32_t gm) {
-  using C = LinCfg<BM, BN, WM, WN>;
-  using E = Elem16<BF>;
+  using C = LinCfg<BM, BN, WM, WN, NS>;
   constexpr int TI = WM / 32, TJ = WN / 32;
   extern __shared__ __attribute__((aligned(1024))) uint8_t lin_smem[];
   __shared__ float s_rs[BM];
@@ -63,60 +106,134 @@ linear_tile_kernel(LinearArgs p, int32_t tiles_n, int32_t gm) {
   xcd_tile(blockIdx.x, gridDim.x, tiles_n, gm, &tm, &tn);
   const int64_t m0 = (int64_t)tm * BM;
   const int32_t n0 = tn * BN;
-  const int nk = (p.K + kLinStage - 1) / kLinStage;
-  const int tail = p.K % kLinStage ? (p.K % kLinStage) / 16 : 8;         // chunks of the last stage
+  const int nkf = p.K / kLinStage, nk = (p.K + kLinStage - 1) / kLinStage;   // whole stages, stages
+  const int tail = (p.K % kLinStage) / 16;                                  // 16-byte chunks of a last, part stage
 
   // Direct load j of this wave covers 8 rows x 128 bytes of block blk; rows past
   // the edge re-read the last one, chunks past the contraction the last one.
   const int8_t* a_tile = p.x + m0 * p.ldx;
   const int8_t* b_tile = p.w + (int64_t)n0 * p.K;
-  auto issue = [&](int st) {
-    uint8_t* base = lin_smem + (st & 1) * C::kStage;
-    const int last_chunk = st == nk - 1 ? tail - 1 : 7;
+  uint32_t voff[C::kLPW];
+  auto chunk_of = [&](int j) { return (lane & 7) ^ (4 * ((w * C::kLPW + j) & 1) + (lane >> 4)); };
 #pragma unroll
-    for (int j = 0; j < C::kLPW; ++j) {
-      const int blk = w * C::kLPW + j;
-      const bool is_a = blk < C::kABlocks;
-      const int row = 8 * (is_a ? blk : blk - C::kABlocks) + (lane >> 3);
-      const int chunk = min((lane & 7) ^ ((row >> 1) & 7), last_chunk);
-      const int64_t last = is_a ? p.M - 1 - m0 : (int64_t)p.N - 1 - n0;
-      const int64_t off = min((int64_t)row, last) * (is_a ? p.ldx : (int64_t)p.K) + 16 * chunk;
-      const int8_t* src = (is_a ? a_tile : b_tile) + (int64_t)st * kLinStage + off;
-      __builtin_amdgcn_global_load_lds((lin_glb_t*)src, (lin_lds_t*)(base + blk * 1024), 16, 0, 0);
-    }
-  };
-  issue(0);
-  for (int i = tid; i < BM + BN; i += C::kThreads) {
-    if (i < BM) s_rs[i] = p.sx[min(m0 + i, p.M - 1)];
-    else s_cs[i - BM] = p.sw[min(n0 + i - BM, p.N - 1)];
+  for (int j = 0; j < C::kLPW; ++j) {
+    const int blk = w * C::kLPW + j;
+    const bool is_a = blk < C::kABlocks;
+    const int row = 8 * (is_a ? blk : blk - C::kABlocks) + (lane >> 3);
+    const int64_t last = is_a ? p.M - 1 - m0 : (int64_t)p.N - 1 - n0;
+    voff[j] = (uint32_t)(min((int64_t)row, last) * (is_a ? p.ldx : (int64_t)p.K) + 16 * chunk_of(j));
   }
+  static_assert(C::kABlocks % 2 == 0, "a block's parity is its load's");
+  auto issue_one = [&](int st, int j) {
+    uint8_t* base = lin_smem + (st % NS) * C::kStage;
+    const int blk = w * C::kLPW + j;
+    const uint32_t back = st < nkf ? 0u : 16u * (uint32_t)max(chunk_of(j) - (tail - 1), 0);
+    const int8_t* src = (blk < C::kABlocks ? a_tile : b_tile) + (int64_t)st * kLinStage + (voff[j] - back);
+    __builtin_amdgcn_global_load_lds((lin_glb_t*)src, (lin_lds_t*)(base + blk * 1024), 16, 0, 0);
+  };
+  auto issue = [&](int st) {
+#pragma unroll
+    for (int j = 0; j < C::kLPW; ++j) issue_one(st, j);
+  };
+
+  // Scales first, into registers: their wait then leaves the stage loads in flight.
+  constexpr int SPT = (BM + BN + C::kThreads - 1) / C::kThreads;
+  float sv[SPT];
+#pragma unroll
+  for (int q = 0; q < SPT; ++q) {
+    const int i = tid + q * C::kThreads;
+    sv[q] = i < BM ? p.sx[min(m0 + i, p.M - 1)] : p.sw[min(n0 + i - BM, p.N - 1)];
+  }
+#pragma unroll
+  for (int st = 0; st < NS - 1; ++st)
+    if (st < nk) issue(st);
+#pragma unroll
+  for (int q = 0; q < SPT; ++q) {
+    const int i = tid + q * C::kThreads;
+    if (i < BM) s_rs[i] = sv[q];
+    else if (i < BM + BN) s_cs[i - BM] = sv[q];
+  }
+
   i32x16 acc[TI][TJ];
 #pragma unroll
   for (int i = 0; i < TI; ++i)
 #pragma unroll
     for (int j = 0; j < TJ; ++j) acc[i][j] = i32x16{};
-  for (int kt = 0; kt < nk; ++kt) {
-    lin_wait_barrier<0>();                       // stage kt landed, everyone is past stage kt - 1
-    if (kt + 1 < nk) issue(kt + 1);
-    const uint8_t* sa = lin_smem + (kt & 1) * C::kStage;
+  i32x4 af[2][TI], bf[2][TJ];
+  // Fragment q of a step: A's first, all of B's, A's others -- the products'
+  // order (i outer, j inner) needs them so.
+  auto read_one = [&](int st, int kk, int q) {
+    const uint8_t* sa = lin_smem + (st % NS) * C::kStage;
     const uint8_t* sb = sa + C::kABlocks * 1024;
-    const int valid = kt == nk - 1 ? tail : 8;
+    if (q == 0 || q > TJ) {
+      const int i = q == 0 ? 0 : q - TJ;
+      af[kk & 1][i] = *reinterpret_cast<const i32x4*>(sa + lin_slot(wm * WM + 32 * i + l32, 2 * kk + hl));
+    } else {
+      bf[kk & 1][q - 1] = *reinterpret_cast<const i32x4*>(sb + lin_slot(wn * WN + 32 * (q - 1) + l32, 2 * kk + hl));
+    }
+  };
+  auto product = [&](int kk, int t) {
+    const int i = t / TJ, j = t % TJ;
+    acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(bf[kk & 1][j], af[kk & 1][i], acc[i][j], 0, 0, 0);
+  };
+  // One step: its products, with the next step's reads behind the first of
+  // them and, where `st_issue` is a stage, that stage's direct loads behind
+  // each.  The order is pinned.
+  constexpr int NP = TI * TJ, NR = TI + TJ;
+  auto step = [&](int kk, int st_read, bool loads, int st_issue) {
+#pragma unroll
+    for (int t = 0; t < NP; ++t) {
+      product(kk, t);
+#pragma unroll
+      for (int q = 0; q < NR; ++q)
+        if (q * NP / NR / 2 == t || (NR > NP && t == NP - 1 && q * NP / NR / 2 > t)) read_one(st_read, (kk + 1) & 3, q);
+      if (loads)
+#pragma unroll
+        for (int j = 0; j < C::kLPW; ++j)
+          if (j * NP / C::kLPW == t) issue_one(st_issue, j);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+
+  // Waiting for stage s (its loads landed, every wave is past stage s - 1)
+  // frees slot (s - 1) % NS for stage s + NS - 1.
+  lin_wait_stage<C::kLPW, NS - 2>(nk - 1);
+  if (NS - 1 < nk) issue(NS - 1);
+#pragma unroll
+  for (int q = 0; q < NR; ++q) read_one(0, 0, q);
+  int kt = 0;
+  for (; kt + NS < nk; ++kt) {
+    __builtin_amdgcn_sched_barrier(0);
+    step(0, kt, false, 0);
+    step(1, kt, false, 0);
+    step(2, kt, false, 0);
+    lin_wait_barrier<(NS - 2) * C::kLPW>();
+    __builtin_amdgcn_sched_barrier(0);
+    step(3, kt + 1, true, kt + NS);
+  }
+  // nothing left to load (and after the last stage an unused read of a slot)
+  for (; kt < nkf; ++kt) {
+    __builtin_amdgcn_sched_barrier(0);
+    step(0, kt, false, 0);
+    step(1, kt, false, 0);
+    step(2, kt, false, 0);
+    lin_wait_stage<C::kLPW, NS - 2>(nk - 2 - kt);
+    __builtin_amdgcn_sched_barrier(0);
+    step(3, kt + 1, false, 0);
+  }
+  if (nkf < nk) {
+    // The part stage: chunks past the contraction hold copies; A's are made 0.
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk) {
-      i32x4 af[TI], bf[TJ];
+      if (2 * kk >= tail) break;
+      if (kk > 0)
 #pragma unroll
-      for (int i = 0; i < TI; ++i) {
-        af[i] = *reinterpret_cast<const i32x4*>(sa + lin_slot(wm * WM + 32 * i + l32, 2 * kk + hl));
-        if (2 * kk + hl >= valid) af[i] = i32x4{0, 0, 0, 0};     // past the contraction: adds nothing
-      }
+        for (int q = 0; q < NR; ++q) read_one(nkf, kk, q);
+      if (2 * kk + hl >= tail)
 #pragma unroll
-      for (int j = 0; j < TJ; ++j)
-        bf[j] = *reinterpret_cast<const i32x4*>(sb + lin_slot(wn * WN + 32 * j + l32, 2 * kk + hl));
+        for (int i = 0; i < TI; ++i) af[kk & 1][i] = i32x4{0, 0, 0, 0};
 #pragma unroll
-      for (int i = 0; i < TI; ++i)
-#pragma unroll
-        for (int j = 0; j < TJ; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(bf[j], af[i], acc[i][j], 0, 0, 0);
+      for (int t = 0; t < NP; ++t) product(kk, t);
     }
   }
   lin_wait_barrier<0>();
@@ -148,38 +265,181 @@ linear_tile_kernel(LinearArgs p, int32_t tiles_n, int32_t gm) {
       float v[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = ost[row * C::kOutLd + c8 + e];
-      if (p.vec && n + 8 <= p.N) {
-        float b[8];
-        if (p.bias) {
-          E::unpack(*reinterpret_cast<const i32x4*>(reinterpret_cast<const uint16_t*>(p.bias) + n), b);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = add_rn(v[e], b[e]);
-        }
-        if (p.residual) {
-          E::unpack(*reinterpret_cast<const i32x4*>(reinterpret_cast<const uint16_t*>(p.residual) + m * p.ldr + n), b);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = add_rn(v[e], b[e]);
-        }
-        *reinterpret_cast<i32x4*>(reinterpret_cast<uint16_t*>(p.y) + m * p.ldy + n) = E::pack(v);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          if (n + e >= p.N) continue;
-          float o = v[e];
-          if (p.bias) o = add_rn(o, E::get(p.bias, n + e));
-          if (p.residual) o = add_rn(o, E::get(p.residual, m * p.ldr + n + e));
-          E::put(p.y, m * p.ldy + n + e, o);
-        }
-      }
+      lin_store<BF>(p, m, n, v);
     }
     asm volatile("" ::: "memory");
   }
 }
 
-template <int BM, int BN, int WM, int WN>
+// ---------------------------------------------------------------------------
+// Few tiles: BM x BN outputs per workgroup, its NW waves taking the stages in
+// turn (wave w stages w, w + NW, ...), each over the whole tile with a private
+// ring of NS stages in LDS -- no barrier until the exact partial sums meet, and
+// a stage's fragments are all read at once.  (Waves that share one tile's
+// stages step by step pay an LDS latency per 32-byte step and a barrier per
+// stage: 128 x 3584 x 9856 25.4 us in 64 x 64 tiles, 17.7 here in 64 x 32 ones.)
+// Loads stay direct-to-LDS ones, eight lanes to a row's 128-byte line: a
+// fragment straight from memory has a row per lane, so neighbouring lanes hit
+// different lines (32 x 3584 x 9856: 18.5 us so, 11.0 here).  Products are v_mfma_i32_16x16x64_i8 (lane l: row l % 16 and
+// chunk l / 16 of its operand; output: column 4 (l / 16) + v of the first
+// operand's rows, row l % 16 of the second's).
+// ---------------------------------------------------------------------------
+template <int N>
+__device__ __forceinline__ void lin_wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+template <int LPW, int R>
+__device__ __forceinline__ void lin_wait_own(int rem) {
+  if constexpr (R == 0) {
+    lin_wait_loads<0>();
+  } else {
+    if (rem >= R) lin_wait_loads<R * LPW>();
+    else lin_wait_own<LPW, R - 1>(rem);
+  }
+}
+
+template <int BM, int BN, int NW, int NS>
+struct SplitCfg {
+  static constexpr int kThreads = 64 * NW;
+  static constexpr int kLoads = (BM + BN) / 8;                 // 1 KB direct loads per stage
+  static constexpr int kStage = kLoads * 1024;
+  static constexpr int kOutLd = BN + 4;                        // staged int32 row
+  static constexpr int kOut = BM * kOutLd * 4;
+  static constexpr int kRing = NS * kStage > kOut ? NS * kStage : kOut;
+  static constexpr size_t kLds = (size_t)NW * kRing;
+};
+
+template <bool BF, int BM, int BN, int NW, int NS>
+__global__ void __launch_bounds__(64 * NW)
+linear_split_kernel(LinearArgs p, int32_t tiles_n, int32_t gm) {
+  using C = SplitCfg<BM, BN, NW, NS>;
+  constexpr int TI = BM / 16, TJ = BN / 16;
+  extern __shared__ __attribute__((aligned(1024))) uint8_t lin_smem[];
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l16 = lane & 15, quad = lane >> 4;
+  int tm, tn;
+  xcd_tile(blockIdx.x, gridDim.x, tiles_n, gm, &tm, &tn);
+  const int64_t m0 = (int64_t)tm * BM;
+  const int32_t n0 = tn * BN;
+  const int nkf = p.K / kLinStage, nk = (p.K + kLinStage - 1) / kLinStage;
+  const int tail = (p.K % kLinStage) / 16;
+  const int mine = w < nk ? (nk - 1 - w) / NW + 1 : 0;         // stages of this wave
+
+  // Direct load j covers 8 rows x 128 bytes; rows past the edge re-read the last
+  // one, chunks past the contraction the last one.
+  const int8_t* a_tile = p.x + m0 * p.ldx;
+  const int8_t* b_tile = p.w + (int64_t)n0 * p.K;
+  uint8_t* ring = lin_smem + w * C::kRing;
+  uint32_t voff[C::kLoads];
+#pragma unroll
+  for (int j = 0; j < C::kLoads; ++j) {
+    const bool is_a = j < BM / 8;
+    const int row = 8 * (is_a ? j : j - BM / 8) + (lane >> 3);
+    const int64_t last = is_a ? p.M - 1 - m0 : (int64_t)p.N - 1 - n0;
+    voff[j] = (uint32_t)(min((int64_t)row, last) * (is_a ? p.ldx : (int64_t)p.K));
+  }
+  auto issue = [&](int i) {                                    // this wave's stage i
+    const int st = w + i * NW;
+    const int last_chunk = st < nkf ? 7 : tail - 1;
+    uint8_t* base = ring + (i % NS) * C::kStage;
+#pragma unroll
+    for (int j = 0; j < C::kLoads; ++j) {
+      const int chunk = min((lane & 7) ^ (4 * (j & 1) + (lane >> 4)), last_chunk);
+      const int8_t* src = (j < BM / 8 ? a_tile : b_tile) + (int64_t)st * kLinStage + (voff[j] + 16 * chunk);
+      __builtin_amdgcn_global_load_lds((lin_glb_t*)src, (lin_lds_t*)(base + j * 1024), 16, 0, 0);
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < NS; ++i)
+    if (i < mine) issue(i);
+
+  i32x4 acc[TI][TJ];
+#pragma unroll
+  for (int i = 0; i < TI; ++i)
+#pragma unroll
+    for (int j = 0; j < TJ; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+  for (int i = 0; i < mine; ++i) {
+    lin_wait_own<C::kLoads, NS - 1>(mine - 1 - i);
+    const uint8_t* sa = ring + (i % NS) * C::kStage;
+    const uint8_t* sb = sa + BM * kLinStage;
+    i32x4 af[2][TI], bf[2][TJ];
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+#pragma unroll
+      for (int r = 0; r < TI; ++r) af[kk][r] = *reinterpret_cast<const i32x4*>(sa + lin_slot(16 * r + l16, 4 * kk + quad));
+#pragma unroll
+      for (int c = 0; c < TJ; ++c) bf[kk][c] = *reinterpret_cast<const i32x4*>(sb + lin_slot(16 * c + l16, 4 * kk + quad));
+    }
+    if (w + i * NW >= nkf) {                                   // the part stage: A's chunks past the contraction are 0
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+        for (int r = 0; r < TI; ++r)
+          if (4 * kk + quad >= tail) af[kk][r] = i32x4{0, 0, 0, 0};
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // the slot is read: refill it
+    if (i + NS < mine) issue(i + NS);
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+      for (int r = 0; r < TI; ++r)
+#pragma unroll
+        for (int c = 0; c < TJ; ++c)
+          acc[r][c] = __builtin_amdgcn_mfma_i32_16x16x64_i8(bf[kk][c], af[kk][r], acc[r][c], 0, 0, 0);
+  }
+  // every load of this wave has landed and every read is done: its ring takes its sums
+  int32_t* part = reinterpret_cast<int32_t*>(ring);
+#pragma unroll
+  for (int r = 0; r < TI; ++r)
+#pragma unroll
+    for (int c = 0; c < TJ; ++c)
+      *reinterpret_cast<i32x4*>(part + (16 * r + l16) * C::kOutLd + 16 * c + 4 * quad) = acc[r][c];
+  __syncthreads();
+  constexpr int CPR = BN / 8;
+  for (int t = tid; t < BM * CPR; t += C::kThreads) {
+    const int row = t / CPR, c8 = 8 * (t % CPR);
+    const int64_t m = m0 + row;
+    const int32_t n = n0 + c8;
+    if (m >= p.M || n >= p.N) continue;
+    int32_t sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+    for (int ww = 0; ww < NW; ++ww) {
+      const int32_t* src = reinterpret_cast<const int32_t*>(lin_smem + ww * C::kRing) + row * C::kOutLd + c8;
+      const i32x4 lo = *reinterpret_cast<const i32x4*>(src), hi = *reinterpret_cast<const i32x4*>(src + 4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        sum[e] += lo[e];
+        sum[4 + e] += hi[e];
+      }
+    }
+    const float rs = p.sx[m];
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = mul_rn(mul_rn((float)sum[e], rs), p.sw[min(n + e, p.N - 1)]);
+    lin_store<BF>(p, m, n, v);
+  }
+}
+
+template <int BM, int BN, int NW, int NS>
+static hipError_t launch_linear_split(const LinearArgs& p, hipStream_t s) {
+  using C = SplitCfg<BM, BN, NW, NS>;
+  auto kern = p.dtype == QSVD_BF16 ? linear_split_kernel<true, BM, BN, NW, NS> : linear_split_kernel<false, BM, BN, NW, NS>;
+  if (C::kLds > 65536)
+    if (hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)C::kLds);
+        e != hipSuccess)
+      return e;
+  const int tn = (p.N + BN - 1) / BN;
+  const int64_t tm = (p.M + BM - 1) / BM;
+  KernelScope ks("linear_i8_split", s);
+  QSVD_LAUNCH(ks, kern, dim3((unsigned)(tm * tn)), dim3(C::kThreads), C::kLds, s, p, tn, xcd_group_rows(tm, tn, 32));
+  return hipGetLastError();
+}
+
+template <int BM, int BN, int WM, int WN, int NS>
 static hipError_t launch_linear_tile(const LinearArgs& p, hipStream_t s) {
-  using C = LinCfg<BM, BN, WM, WN>;
-  auto kern = p.dtype == QSVD_BF16 ? linear_tile_kernel<true, BM, BN, WM, WN> : linear_tile_kernel<false, BM, BN, WM, WN>;
+  using C = LinCfg<BM, BN, WM, WN, NS>;
+  auto kern = p.dtype == QSVD_BF16 ? linear_tile_kernel<true, BM, BN, WM, WN, NS>
+                                   : linear_tile_kernel<false, BM, BN, WM, WN, NS>;
   if (C::kLds > 65536 - 4 * (BM + BN))
     if (hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)C::kLds);
         e != hipSuccess)
@@ -191,9 +451,51 @@ static hipError_t launch_linear_tile(const LinearArgs& p, hipStream_t s) {
   return hipGetLastError();
 }
 
+// The forms a product may take, and what each costs.  A compute unit takes
+// q = ceil(tiles / 256) tiles; a tile of nk 128-byte stages then costs about
+// fixed + q (tile + nk stage) microseconds.  The three numbers of a form are
+// fitted to its measured times over 100 products (M 1 .. 8192, N 48 .. 32768,
+// K 128 .. 16384, operands from HBM); the form with the least estimate was on
+// average 1.4% and at most 24% slower than the best of 18 forms measured.  What
+// they express: a unit takes in at most 55 to 60 bytes per ns while weights
+// come from HBM (95 if everything were in L2), so the stage times are those of
+// (BM + BN) 128 bytes except for the two largest tiles, which the products
+// bound; small tiles have the shorter ramp and epilogue.
+struct LinForm {
+  int32_t bm, bn;
+  double fixed, tile, stage;
+  int64_t max_m;            // the few-rows forms repeat the weights beyond it
+  hipError_t (*launch)(const LinearArgs&, hipStream_t);
+};
+static const LinForm kLinForms[] = {
+    {16, 16, 1.499, 1.137, 0.050, 16, launch_linear_split<16, 16, 8, 2>},
+    {32, 16, 1.870, 0.717, 0.070, 32, launch_linear_split<32, 16, 8, 1>},
+    {32, 32, 1.100, 1.547, 0.089, 32, launch_linear_split<32, 32, 8, 1>},
+    {64, 16, 1.870, 1.069, 0.103, 2048, launch_linear_split<64, 16, 8, 1>},
+    {64, 32, 0.334, 2.804, 0.131, 2048, launch_linear_split<64, 32, 8, 1>},
+    {64, 64, 0.000, 4.123, 0.185, 2048, launch_linear_split<64, 64, 4, 2>},
+    {64, 64, 1.930, 1.665, 0.257, INT64_MAX, launch_linear_tile<64, 64, 32, 32, 4>},
+    {64, 128, 1.822, 2.218, 0.408, INT64_MAX, launch_linear_tile<64, 128, 32, 64, 3>},
+    {128, 128, 0.000, 4.531, 0.519, INT64_MAX, launch_linear_tile<128, 128, 64, 32, 4>},
+    {128, 256, 0.000, 5.414, 0.860, INT64_MAX, launch_linear_tile<128, 256, 64, 64, 3>},
+    {192, 256, 0.000, 6.006, 1.333, INT64_MAX, launch_linear_tile<192, 256, 96, 64, 2>},
+    {256, 256, 0.000, 6.823, 1.479, INT64_MAX, launch_linear_tile<256, 256, 128, 64, 2>},
+};
+constexpr int64_t kLinUnits = 256;            // compute units
+constexpr int64_t kLinMaxTiles = 1 << 23;     // fewer than 2^32 threads of up to 512 per tile
+
 hipError_t launch_linear_i8(const LinearArgs& p, hipStream_t s) {
   if (p.M == 0) return hipSuccess;
-  return launch_linear_tile<128, 128, 64, 64>(p, s);
+  const LinForm* best = nullptr;
+  double least = 0.0;
+  const double nk = (double)((p.K + kLinStage - 1) / kLinStage);
+  for (const LinForm& f : kLinForms) {
+    const int64_t tiles = ((p.M + f.bm - 1) / f.bm) * (((int64_t)p.N + f.bn - 1) / f.bn);
+    if (p.M > f.max_m || tiles >= kLinMaxTiles) continue;
+    const double q = (double)((tiles + kLinUnits - 1) / kLinUnits), us = f.fixed + q * (f.tile + nk * f.stage);
+    if (!best || us < least) best = &f, least = us;
+  }
+  return best ? best->launch(p, s) : hipErrorInvalidConfiguration;
 }
 
 }  // namespace qsvd
