@@ -211,9 +211,15 @@ def ptr(t):
 
 
 def stream_handle(stream=None):
+    """The hipStream_t of a torch stream, by default the current device's
+    current stream (read without building a stream object: 3 us of a call's 7
+    were spent on that)."""
     import torch
-    s = torch.cuda.current_stream() if stream is None else stream
-    return s.cuda_stream
+    if stream is not None:
+        return stream.cuda_stream
+    if not torch.cuda.is_initialized():
+        torch.cuda.init()
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 class DeviceLayer:
