@@ -6,10 +6,10 @@
 //   gate   y = silu(g) * u, Q(y)
 //
 // Both are bound by memory: a norm reads 2 or 4 bytes and writes 1 to 5 per
-// element for some ten operations.  A workgroup holds a whole row in
-// registers (a thread the 8-element chunks tid, tid + T, ...), so every element
-// is read and written once; the row's sum of squares and largest |y| go round
-// the workgroup through LDS.
+// element for some ten operations.  A workgroup holds one row in registers
+// (a thread the 8-element chunks tid, tid + T, ...), so every element is read
+// and written once; the row's sum of squares and largest |y| go round its waves
+// (through LDS if there are several).
 #include "common.h"
 #include "elem16.h"
 #include "launch.h"
@@ -31,11 +31,13 @@ __device__ __forceinline__ RowScale row_scale(float amax, float clip, float qm) 
   return RowScale{div_rn(qm, a), div_rn(a, qm)};
 }
 
-// Codes of 8 values at chunk c of the row's codes.
+// Codes of 8 values at chunk c of the row's codes.  (A row whose codes are 0
+// may hold values that are not finite: 0 times those is not 0.)
 __device__ __forceinline__ void store_codes(uint8_t* row, int c, const float* y, float inv, float qm, int32_t bits) {
-  uint32_t q[8];
+  uint32_t q[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  if (inv != 0.f)
 #pragma unroll
-  for (int e = 0; e < 8; ++e) q[e] = inv == 0.f ? 0u : code_bits(y[e], inv, qm);
+    for (int e = 0; e < 8; ++e) q[e] = code_bits(y[e], inv, qm);
   if (bits == 8)
     *reinterpret_cast<uint2*>(row + 8 * c) =
         make_uint2(pack4_codes8(q[0], q[1], q[2], q[3]), pack4_codes8(q[4], q[5], q[6], q[7]));
@@ -46,79 +48,89 @@ __device__ __forceinline__ void store_codes(uint8_t* row, int c, const float* y,
 // Larger of two magnitudes, NaN if either is.
 __device__ __forceinline__ float max_nan(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 
-__device__ __forceinline__ float block_max(float v, float* part) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = max_nan(v, __shfl_xor(v, o, kWave));
+// Exchanges within 16 lanes without LDS: neighbours, pairs, mirrored quads and
+// mirrored halves (whose lanes agree by then).
+template <int CTRL>
+__device__ __forceinline__ float dpp(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
+}
+template <int CTRL>
+__device__ __forceinline__ double dpp(double x) {
+  const uint2 v = __builtin_bit_cast(uint2, x);
+  return __builtin_bit_cast(double, make_uint2(__builtin_amdgcn_update_dpp(0, (int)v.x, CTRL, 0xf, 0xf, true),
+                                               __builtin_amdgcn_update_dpp(0, (int)v.y, CTRL, 0xf, 0xf, true)));
+}
+
+// f of all threads' v; `part` holds a value per wave.
+template <class T, class F>
+__device__ __forceinline__ T row_reduce(T v, F f, T* part) {
+  v = f(v, dpp<0xB1>(v));
+  v = f(v, dpp<0x4E>(v));
+  v = f(v, dpp<0x141>(v));
+  v = f(v, dpp<0x140>(v));
+  v = f(v, __shfl_xor(v, 16, kWave));
+  v = f(v, __shfl_xor(v, 32, kWave));
   const int nw = blockDim.x >> 6;
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = part[0];
-  for (int w = 1; w < nw; ++w) v = max_nan(v, part[w]);
+  if (nw > 1) {
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = part[0];
+    for (int w = 1; w < nw; ++w) v = f(v, part[w]);
+  }
   return v;
 }
 
-__device__ __forceinline__ double block_sum(double v, double* part) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
-  const int nw = blockDim.x >> 6;
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = part[0];
-  for (int w = 1; w < nw; ++w) v += part[w];
-  return v;
-}
-
-// One row per workgroup, at most MAXC chunks per thread.  The squares of
-// 16-bit values are exact in fp64 and are added there, so the order of the
-// sum practically never reaches r = fl32(1 / sqrt(mean + eps)): codes are a
-// function of the row, not of the launch.
+// One row per workgroup, at most MAXC chunks per thread.  The squares of 16-bit
+// values are exact in fp64 and are added there, so the order
+// of the sum practically never reaches r = fl32(1 / sqrt(mean + eps)): codes
+// are a function of the row, not of the launch.
 template <bool BF, int MAXC>
 __global__ void __launch_bounds__(64 * kRowMaxWaves)
 rmsnorm_quantize_kernel(NormArgs a) {
   using E = Elem16<BF>;
   __shared__ double s_sum[kRowMaxWaves];
   __shared__ float s_max[kRowMaxWaves];
-  const int tid = threadIdx.x, nt = blockDim.x;
+  const int tid = threadIdx.x, NT = blockDim.x;
   const int64_t m = blockIdx.x;
   const int nch = a.K >> 3;
   const uint16_t* x = reinterpret_cast<const uint16_t*>(a.x) + m * a.ldx;
-  const uint16_t* res = reinterpret_cast<const uint16_t*>(a.residual) + m * a.ldr;
   const uint16_t* gamma = reinterpret_cast<const uint16_t*>(a.gamma);
-  i32x4 hv[MAXC], gv[MAXC];
+  i32x4 hv[MAXC], rv[MAXC], gv[MAXC];
 #pragma unroll
   for (int i = 0; i < MAXC; ++i) {
-    const int c = tid + nt * i;
-    hv[i] = gv[i] = i32x4{0, 0, 0, 0};
-    if (c < nch) {
-      hv[i] = *reinterpret_cast<const i32x4*>(x + 8 * c);
-      gv[i] = *reinterpret_cast<const i32x4*>(gamma + 8 * c);
-    }
+    const int c = tid + NT * i;
+    hv[i] = rv[i] = gv[i] = i32x4{0, 0, 0, 0};
+    if (c < nch) hv[i] = *reinterpret_cast<const i32x4*>(x + 8 * c);
   }
   if (a.residual) {
+    const uint16_t* res = reinterpret_cast<const uint16_t*>(a.residual) + m * a.ldr;
 #pragma unroll
-    for (int i = 0; i < MAXC; ++i) {
-      const int c = tid + nt * i;
-      if (c >= nch) continue;
-      float f[8], g[8];
-      E::unpack(hv[i], f);
-      E::unpack(*reinterpret_cast<const i32x4*>(res + 8 * c), g);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) f[e] = add_rn(f[e], g[e]);
-      hv[i] = E::pack(f);
-    }
+    for (int i = 0; i < MAXC; ++i)
+      if (tid + NT * i < nch) rv[i] = *reinterpret_cast<const i32x4*>(res + 8 * (tid + NT * i));
   }
+#pragma unroll
+  for (int i = 0; i < MAXC; ++i)
+    if (tid + NT * i < nch) gv[i] = *reinterpret_cast<const i32x4*>(gamma + 8 * (tid + NT * i));
   double ss = 0.0;
 #pragma unroll
   for (int i = 0; i < MAXC; ++i) {
-    const int c = tid + nt * i;
-    if (c >= nch) continue;
-    if (a.h) *reinterpret_cast<i32x4*>(reinterpret_cast<uint16_t*>(a.h) + m * a.ldh + 8 * c) = hv[i];
     float f[8];
     E::unpack(hv[i], f);
+    if (a.residual) {
+      float g[8];
+      E::unpack(rv[i], g);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] = add_rn(f[e], g[e]);
+      hv[i] = E::pack(f);
+      E::unpack(hv[i], f);
+    }
+    if (a.h && tid + NT * i < nch)
+      *reinterpret_cast<i32x4*>(reinterpret_cast<uint16_t*>(a.h) + m * a.ldh + 8 * (tid + NT * i)) = hv[i];
 #pragma unroll
     for (int e = 0; e < 8; ++e) ss = fma((double)f[e], (double)f[e], ss);
+    __builtin_amdgcn_sched_barrier(0);
   }
-  ss = block_sum(ss, s_sum);
+  ss = row_reduce(ss, [](double p, double q) { return p + q; }, s_sum);
   const float r = (float)(1.0 / sqrt(ss / a.K + (double)a.eps));
   float y[MAXC][8];
   float amax = 0.f;
@@ -129,25 +141,27 @@ rmsnorm_quantize_kernel(NormArgs a) {
     E::unpack(gv[i], g);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      y[i][e] = mul_rn(mul_rn(f[e], r), g[e]);
-      if (tid + nt * i < nch) amax = max_nan(amax, fabsf(y[i][e]));
+      y[i][e] = mul_rn(mul_rn(f[e], r), g[e]);        // (an absent chunk's are 0, or NaN with the row)
+      amax = max_nan(amax, fabsf(y[i][e]));
     }
+    __builtin_amdgcn_sched_barrier(0);                // one chunk at a time: few live registers
   }
   if (a.y)
 #pragma unroll
     for (int i = 0; i < MAXC; ++i) {
-      const int c = tid + nt * i;
+      const int c = tid + NT * i;
       if (c < nch) *reinterpret_cast<i32x4*>(reinterpret_cast<uint16_t*>(a.y) + m * a.ldy + 8 * c) = E::pack(y[i]);
     }
   if (!a.xq) return;
   const float qm = (float)((1 << (a.bits - 1)) - 1);
-  const RowScale sc = row_scale(block_max(amax, s_max), a.clip, qm);
+  const RowScale sc = row_scale(row_reduce(amax, max_nan, s_max), a.clip, qm);
   if (tid == 0) a.sx[m] = sc.s;
-  uint8_t* row = (uint8_t*)a.xq + m * (int64_t)(a.bits == 8 ? a.K : a.K / 2);
+  uint8_t* codes = (uint8_t*)a.xq + m * (int64_t)(a.bits == 8 ? a.K : a.K / 2);
 #pragma unroll
   for (int i = 0; i < MAXC; ++i) {
-    const int c = tid + nt * i;
-    if (c < nch) store_codes(row, c, y[i], sc.inv, qm, a.bits);
+    const int c = tid + NT * i;
+    if (c < nch) store_codes(codes, c, y[i], sc.inv, qm, a.bits);
+    __builtin_amdgcn_sched_barrier(0);
   }
 }
 
@@ -169,7 +183,7 @@ __global__ void __launch_bounds__(64 * kRowMaxWaves)
 silu_mul_quantize_kernel(GateArgs a) {
   using E = Elem16<BF>;
   __shared__ float s_max[kRowMaxWaves];
-  const int tid = threadIdx.x, nt = blockDim.x;
+  const int tid = threadIdx.x, NT = blockDim.x;
   const int64_t m = blockIdx.x;
   const int nch = a.K >> 3;
   const uint16_t* gate = reinterpret_cast<const uint16_t*>(a.gate) + m * a.ldg;
@@ -177,7 +191,7 @@ silu_mul_quantize_kernel(GateArgs a) {
   i32x4 gv[MAXC], uv[MAXC];
 #pragma unroll
   for (int i = 0; i < MAXC; ++i) {
-    const int c = tid + nt * i;
+    const int c = tid + NT * i;
     gv[i] = uv[i] = i32x4{0, 0, 0, 0};
     if (c < nch) {
       gv[i] = *reinterpret_cast<const i32x4*>(gate + 8 * c);
@@ -196,47 +210,58 @@ silu_mul_quantize_kernel(GateArgs a) {
       y[i][e] = silu(g[e]) * u[e];
       amax = max_nan(amax, fabsf(y[i][e]));
     }
+    __builtin_amdgcn_sched_barrier(0);
   }
   const float qm = (float)((1 << (a.bits - 1)) - 1);
-  const RowScale sc = row_scale(block_max(amax, s_max), a.clip, qm);
+  const RowScale sc = row_scale(row_reduce(amax, max_nan, s_max), a.clip, qm);
   if (tid == 0) a.sx[m] = sc.s;
-  uint8_t* row = (uint8_t*)a.xq + m * (int64_t)(a.bits == 8 ? a.K : a.K / 2);
+  uint8_t* codes = (uint8_t*)a.xq + m * (int64_t)(a.bits == 8 ? a.K : a.K / 2);
 #pragma unroll
   for (int i = 0; i < MAXC; ++i) {
-    const int c = tid + nt * i;
-    if (c < nch) store_codes(row, c, y[i], sc.inv, qm, a.bits);
+    const int c = tid + NT * i;
+    if (c < nch) store_codes(codes, c, y[i], sc.inv, qm, a.bits);
+    __builtin_amdgcn_sched_barrier(0);
   }
 }
 
-// Threads per row: four chunks each, at least a wave and at most 16 of them
-// (longer rows: up to eight chunks each).
-static int row_threads(int32_t K) {
-  const int waves = (K / 8 + 255) / 256;
-  return 64 * (waves < 1 ? 1 : waves > kRowMaxWaves ? kRowMaxWaves : waves);
+// Waves of a row at MAXC chunks per thread.  Two chunks each fill the registers
+// that eight waves per SIMD leave, and waves beyond the row's chunks would
+// only repeat its reductions: 2560 x 11264 gates take 28.9 us (5.0 TB/s, where
+// a large copy runs at 5.1) at two chunks with the row's own eleven waves, 31.4
+// with sixteen, 30.9 at four chunks; 5632 x 5120 norms 41.3 (4.9 TB/s), 44.6
+// with eight waves for five, 50.6 at one chunk.  Rows of one wave take one chunk
+// (8192 x 256 norms 6.5 us, 7.8 at two); rows past 16 waves of two take four or
+// eight (512 x 32768 gates 19.8 us, 100 x 65536 norms 25.3).
+static int row_threads(int32_t K, int maxc) { return 64 * ((K / 8 + 64 * maxc - 1) / (64 * maxc)); }
+
+template <int MAXC>
+static hipError_t launch_norm(const NormArgs& a, hipStream_t s) {
+  auto kern = a.dtype == QSVD_BF16 ? rmsnorm_quantize_kernel<true, MAXC> : rmsnorm_quantize_kernel<false, MAXC>;
+  KernelScope ks("rmsnorm_quantize", s);
+  QSVD_LAUNCH(ks, kern, dim3((unsigned)a.M), dim3(row_threads(a.K, MAXC)), 0, s, a);
+  return hipGetLastError();
+}
+
+template <int MAXC>
+static hipError_t launch_gate(const GateArgs& a, hipStream_t s) {
+  auto kern = a.dtype == QSVD_BF16 ? silu_mul_quantize_kernel<true, MAXC> : silu_mul_quantize_kernel<false, MAXC>;
+  KernelScope ks("silu_mul_quantize", s);
+  QSVD_LAUNCH(ks, kern, dim3((unsigned)a.M), dim3(row_threads(a.K, MAXC)), 0, s, a);
+  return hipGetLastError();
 }
 
 hipError_t launch_rmsnorm_quantize(const NormArgs& a, hipStream_t s) {
   if (a.M == 0) return hipSuccess;
-  const int nt = row_threads(a.K);
-  const bool few = a.K / 8 <= 4 * nt;
-  const dim3 grid((unsigned)a.M), block(nt);
-  KernelScope ks("rmsnorm_quantize", s);
-  auto kern = a.dtype == QSVD_BF16 ? (few ? rmsnorm_quantize_kernel<true, 4> : rmsnorm_quantize_kernel<true, 8>)
-                                   : (few ? rmsnorm_quantize_kernel<false, 4> : rmsnorm_quantize_kernel<false, 8>);
-  QSVD_LAUNCH(ks, kern, grid, block, 0, s, a);
-  return hipGetLastError();
+  const int ch = a.K / 8;
+  return ch <= 64 ? launch_norm<1>(a, s) : ch <= 2048 ? launch_norm<2>(a, s)
+         : ch <= 4096 ? launch_norm<4>(a, s) : launch_norm<8>(a, s);
 }
 
 hipError_t launch_silu_mul_quantize(const GateArgs& a, hipStream_t s) {
   if (a.M == 0) return hipSuccess;
-  const int nt = row_threads(a.K);
-  const bool few = a.K / 8 <= 4 * nt;
-  const dim3 grid((unsigned)a.M), block(nt);
-  KernelScope ks("silu_mul_quantize", s);
-  auto kern = a.dtype == QSVD_BF16 ? (few ? silu_mul_quantize_kernel<true, 4> : silu_mul_quantize_kernel<true, 8>)
-                                   : (few ? silu_mul_quantize_kernel<false, 4> : silu_mul_quantize_kernel<false, 8>);
-  QSVD_LAUNCH(ks, kern, grid, block, 0, s, a);
-  return hipGetLastError();
+  const int ch = a.K / 8;
+  return ch <= 64 ? launch_gate<1>(a, s) : ch <= 2048 ? launch_gate<2>(a, s)
+         : ch <= 4096 ? launch_gate<4>(a, s) : launch_gate<8>(a, s);
 }
 
 }  // namespace qsvd
