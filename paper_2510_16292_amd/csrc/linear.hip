@@ -1,14 +1,16 @@
 // W8A8 linear layer: int8 x int8 -> int32 on the matrix cores
-// (v_mfma_i32_32x32x32_i8), then in fp32, each step rounded on its own,
+// (v_mfma_i32_16x16x64_i8), then in fp32, each step rounded on its own,
 //   y = (f32(acc) * sx[m]) * sw[n]  (+ bias[n])  (+ residual[m][n])
 // and one rounding to fp16 / bf16 (per-token activations and per-channel
 // weights, Section 4 setup, for the layer's products beside the joint QKV one).
 //
-// Operand layout of one 32x32x32 product: lane l supplies row l % 32 of its
+// Operand layout of one 16x16x64 product: lane l supplies row l % 16 of its
 // operand, 16 contraction bytes; which bytes only has to agree between the
 // two operands (integer sums are exact in any order).  Output: lane l holds
-// row l % 32 of the second operand and columns 8 (v / 4) + 4 (l / 32) + v % 4
-// of the first.
+// row l % 16 of the second operand and rows 4 (l / 16) + 0..3 of the first.
+// (32x32x32 products have the same rate and half the instructions, but cost
+// more power, which is what bounds a long product: 8192^3 449 us with them,
+// 418 with these.)
 #include "common.h"
 #include "elem16.h"
 #include "launch.h"
@@ -32,7 +34,10 @@ __device__ __forceinline__ void lin_wait_barrier() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
-// The same for a stage that `rem` stages (at most R count) were issued after.
+// This wave's LDS reads done (its loads stay in flight), then the barrier.
+__device__ __forceinline__ void lin_read_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// lin_wait_barrier for a stage that `rem` stages (at most R count) were issued after.
 template <int LPW, int R>
 __device__ __forceinline__ void lin_wait_stage(int rem) {
   if constexpr (R == 0) {
@@ -78,30 +83,32 @@ struct LinCfg {
   static constexpr int kWaves = (BM / WM) * (BN / WN);
   static constexpr int kThreads = 64 * kWaves;
   static constexpr int kABlocks = BM / 8, kBBlocks = BN / 8;              // 1 KB direct loads
-  static constexpr int kLPW = (kABlocks + kBBlocks) / kWaves;             // per wave and stage
-  static_assert((kABlocks + kBBlocks) % kWaves == 0, "whole loads per wave");
+  static constexpr int kBlocks = kABlocks + kBBlocks;
+  static constexpr int kLPW = (kBlocks + kWaves - 1) / kWaves;            // per wave and stage
   static constexpr int kStage = (kABlocks + kBBlocks) * 1024;
-  static constexpr int kOutLd = WN + 4;                                   // staged fp32 row, 32 rows a wave
-  static constexpr int kOut = kWaves * 32 * kOutLd * 4;
+  static constexpr int kOutLd = WN + 4;                                   // staged fp32 row, 16 rows a wave
+  static constexpr int kOut = kWaves * 16 * kOutLd * 4;
   static constexpr size_t kLds = NS * kStage > kOut ? NS * kStage : kOut;
 };
 
 // BM x BN outputs per workgroup (WM x WN per wave), the contraction in stages of
-// 128 bytes, NS of them in LDS: NS - 1 stages' direct loads (global memory
-// straight into LDS) are in flight while one is multiplied; one barrier per
-// stage.  The fragments of a 32-byte step are read while the products of the
-// step before run.
+// 128 bytes, NS of them in LDS, whose direct loads (global memory straight into
+// LDS) are in flight while one is multiplied.  A stage is two 64-byte steps; a
+// step's fragments are read under the products of the step before, and the
+// order of products, reads and loads is pinned: left to the compiler, all of a
+// stage's loads go out at once while the matrix cores wait (8192^3 477 us,
+// 443 pinned, both on the 32x32x32 products).
 template <bool BF, int BM, int BN, int WM, int WN, int NS>
 __global__ void __launch_bounds__((LinCfg<BM, BN, WM, WN, NS>::kThreads))
 linear_tile_kernel(LinearArgs p, int32_t tiles_n, int32_t gm) {
   using C = LinCfg<BM, BN, WM, WN, NS>;
-  constexpr int TI = WM / 32, TJ = WN / 32;
+  constexpr int TI = WM / 16, TJ = WN / 16;
   extern __shared__ __attribute__((aligned(1024))) uint8_t lin_smem[];
   __shared__ float s_rs[BM];
   __shared__ __attribute__((aligned(16))) float s_cs[BN];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = w / (BN / WN), wn = w % (BN / WN);
-  const int l32 = lane & 31, hl = lane >> 5;
+  const int lr = lane & 15, lc = lane >> 4;                   // a lane's fragment row and chunk
   int tm, tn;
   xcd_tile(blockIdx.x, gridDim.x, tiles_n, gm, &tm, &tn);
   const int64_t m0 = (int64_t)tm * BM;
@@ -109,24 +116,27 @@ linear_tile_kernel(LinearArgs p, int32_t tiles_n, int32_t gm) {
   const int nkf = p.K / kLinStage, nk = (p.K + kLinStage - 1) / kLinStage;   // whole stages, stages
   const int tail = (p.K % kLinStage) / 16;                                  // 16-byte chunks of a last, part stage
 
-  // Direct load j of this wave covers 8 rows x 128 bytes of block blk; rows past
-  // the edge re-read the last one, chunks past the contraction the last one.
+  // Direct load j of this wave covers 8 rows x 128 bytes of a block; rows past
+  // the edge re-read the last one, chunks past the contraction the last one,
+  // and a wave's loads past the last block repeat that (the same bytes to the
+  // same place).
   const int8_t* a_tile = p.x + m0 * p.ldx;
   const int8_t* b_tile = p.w + (int64_t)n0 * p.K;
   uint32_t voff[C::kLPW];
-  auto chunk_of = [&](int j) { return (lane & 7) ^ (4 * ((w * C::kLPW + j) & 1) + (lane >> 4)); };
+  auto block_of = [&](int j) { return min(w * C::kLPW + j, C::kBlocks - 1); };
+  auto chunk_of = [&](int j) { return (lane & 7) ^ (4 * (block_of(j) & 1) + (lane >> 4)); };
 #pragma unroll
   for (int j = 0; j < C::kLPW; ++j) {
-    const int blk = w * C::kLPW + j;
+    const int blk = block_of(j);
     const bool is_a = blk < C::kABlocks;
     const int row = 8 * (is_a ? blk : blk - C::kABlocks) + (lane >> 3);
     const int64_t last = is_a ? p.M - 1 - m0 : (int64_t)p.N - 1 - n0;
     voff[j] = (uint32_t)(min((int64_t)row, last) * (is_a ? p.ldx : (int64_t)p.K) + 16 * chunk_of(j));
   }
-  static_assert(C::kABlocks % 2 == 0, "a block's parity is its load's");
+  static_assert(C::kABlocks % 2 == 0, "a block's parity is that of its rows");
   auto issue_one = [&](int st, int j) {
     uint8_t* base = lin_smem + (st % NS) * C::kStage;
-    const int blk = w * C::kLPW + j;
+    const int blk = block_of(j);
     const uint32_t back = st < nkf ? 0u : 16u * (uint32_t)max(chunk_of(j) - (tail - 1), 0);
     const int8_t* src = (blk < C::kABlocks ? a_tile : b_tile) + (int64_t)st * kLinStage + (voff[j] - back);
     __builtin_amdgcn_global_load_lds((lin_glb_t*)src, (lin_lds_t*)(base + blk * 1024), 16, 0, 0);
@@ -154,11 +164,11 @@ linear_tile_kernel(LinearArgs p, int32_t tiles_n, int32_t gm) {
     else if (i < BM + BN) s_cs[i - BM] = sv[q];
   }
 
-  i32x16 acc[TI][TJ];
+  i32x4 acc[TI][TJ];
 #pragma unroll
   for (int i = 0; i < TI; ++i)
 #pragma unroll
-    for (int j = 0; j < TJ; ++j) acc[i][j] = i32x16{};
+    for (int j = 0; j < TJ; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
   i32x4 af[2][TI], bf[2][TJ];
   // Fragment q of a step: A's first, all of B's, A's others -- the products'
   // order (i outer, j inner) needs them so.
@@ -167,26 +177,28 @@ linear_tile_kernel(LinearArgs p, int32_t tiles_n, int32_t gm) {
     const uint8_t* sb = sa + C::kABlocks * 1024;
     if (q == 0 || q > TJ) {
       const int i = q == 0 ? 0 : q - TJ;
-      af[kk & 1][i] = *reinterpret_cast<const i32x4*>(sa + lin_slot(wm * WM + 32 * i + l32, 2 * kk + hl));
+      af[kk][i] = *reinterpret_cast<const i32x4*>(sa + lin_slot(wm * WM + 16 * i + lr, 4 * kk + lc));
     } else {
-      bf[kk & 1][q - 1] = *reinterpret_cast<const i32x4*>(sb + lin_slot(wn * WN + 32 * (q - 1) + l32, 2 * kk + hl));
+      bf[kk][q - 1] = *reinterpret_cast<const i32x4*>(sb + lin_slot(wn * WN + 16 * (q - 1) + lr, 4 * kk + lc));
     }
   };
   auto product = [&](int kk, int t) {
     const int i = t / TJ, j = t % TJ;
-    acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(bf[kk & 1][j], af[kk & 1][i], acc[i][j], 0, 0, 0);
+    acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(bf[kk][j], af[kk][i], acc[i][j], 0, 0, 0);
   };
-  // One step: its products, with the next step's reads behind the first of
-  // them and, where `st_issue` is a stage, that stage's direct loads behind
-  // each.  The order is pinned.
+  // One step: its products, with the next step's reads behind the first half of
+  // them and, on a stage's last step, a later stage's direct loads behind all.
+  // The order is pinned.
   constexpr int NP = TI * TJ, NR = TI + TJ;
+  constexpr bool kMid = NS == 2;
+  static_assert(!kMid || NP % 2 == 0, "halves");
   auto step = [&](int kk, int st_read, bool loads, int st_issue) {
 #pragma unroll
     for (int t = 0; t < NP; ++t) {
       product(kk, t);
 #pragma unroll
       for (int q = 0; q < NR; ++q)
-        if (q * NP / NR / 2 == t || (NR > NP && t == NP - 1 && q * NP / NR / 2 > t)) read_one(st_read, (kk + 1) & 3, q);
+        if (q * NP / NR / 2 == t || (NR > NP && t == NP - 1 && q * NP / NR / 2 > t)) read_one(st_read, 1 - kk, q);
       if (loads)
 #pragma unroll
         for (int j = 0; j < C::kLPW; ++j)
@@ -195,71 +207,112 @@ linear_tile_kernel(LinearArgs p, int32_t tiles_n, int32_t gm) {
     }
   };
 
-  // Waiting for stage s (its loads landed, every wave is past stage s - 1)
-  // frees slot (s - 1) % NS for stage s + NS - 1.
-  lin_wait_stage<C::kLPW, NS - 2>(nk - 1);
-  if (NS - 1 < nk) issue(NS - 1);
-#pragma unroll
-  for (int q = 0; q < NR; ++q) read_one(0, 0, q);
   int kt = 0;
-  for (; kt + NS < nk; ++kt) {
-    __builtin_amdgcn_sched_barrier(0);
-    step(0, kt, false, 0);
-    step(1, kt, false, 0);
-    step(2, kt, false, 0);
-    lin_wait_barrier<(NS - 2) * C::kLPW>();
-    __builtin_amdgcn_sched_barrier(0);
-    step(3, kt + 1, true, kt + NS);
-  }
-  // nothing left to load (and after the last stage an unused read of a slot)
-  for (; kt < nkf; ++kt) {
-    __builtin_amdgcn_sched_barrier(0);
-    step(0, kt, false, 0);
-    step(1, kt, false, 0);
-    step(2, kt, false, 0);
-    lin_wait_stage<C::kLPW, NS - 2>(nk - 2 - kt);
-    __builtin_amdgcn_sched_barrier(0);
-    step(3, kt + 1, false, 0);
+  if constexpr (kMid) {
+    // Two stages only: a stage's slot is refilled from the middle of its
+    // first step on (all of it is read by then) instead of from its second, for
+    // a second barrier (2560 x 4096 x 11264 in 192 x 256 tiles 123.6 -> 120.4 us).
+    constexpr int H = NP / 2;
+    auto half = [&](int kk, int h, int st_read, int read_kk, int st_issue) {
+#pragma unroll
+      for (int t = h * H; t < (h + 1) * H; ++t) {
+        product(kk, t);
+        if (st_read >= 0)
+#pragma unroll
+          for (int q = 0; q < NR; ++q)
+            if (q * H / NR == t - h * H) read_one(st_read, read_kk, q);
+        if (st_issue >= 0)
+#pragma unroll
+          for (int j = 0; j < C::kLPW; ++j)
+            if (j * H / C::kLPW == t - h * H) issue_one(st_issue, j);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    if (1 < nk) issue(1);
+    lin_wait_stage<C::kLPW, 1>(nk - 1);
+#pragma unroll
+    for (int q = 0; q < NR; ++q) read_one(0, 0, q);
+    for (; kt + 2 < nk; ++kt) {
+      __builtin_amdgcn_sched_barrier(0);
+      half(0, 0, kt, 1, -1);
+      lin_read_barrier();
+      __builtin_amdgcn_sched_barrier(0);
+      half(0, 1, -1, 0, kt + 2);
+      half(1, 0, -1, 0, -1);
+      lin_wait_barrier<C::kLPW>();
+      __builtin_amdgcn_sched_barrier(0);
+      half(1, 1, kt + 1, 0, -1);
+    }
+    // nothing left to load (and after the last stage an unused read of a slot)
+    for (; kt < nkf; ++kt) {
+      __builtin_amdgcn_sched_barrier(0);
+      half(0, 0, kt, 1, -1);
+      half(0, 1, -1, 0, -1);
+      half(1, 0, -1, 0, -1);
+      lin_wait_barrier<0>();
+      __builtin_amdgcn_sched_barrier(0);
+      half(1, 1, kt + 1, 0, -1);
+    }
+  } else {
+    // Waiting for stage s (its loads landed, every wave is past stage s - 1)
+    // frees slot (s - 1) % NS for stage s + NS - 1.
+    lin_wait_stage<C::kLPW, NS - 2>(nk - 1);
+    if (NS - 1 < nk) issue(NS - 1);
+#pragma unroll
+    for (int q = 0; q < NR; ++q) read_one(0, 0, q);
+    for (; kt + NS < nk; ++kt) {
+      __builtin_amdgcn_sched_barrier(0);
+      step(0, kt, false, 0);
+      lin_wait_barrier<(NS - 2) * C::kLPW>();
+      __builtin_amdgcn_sched_barrier(0);
+      step(1, kt + 1, true, kt + NS);
+    }
+    // nothing left to load (and after the last stage an unused read of a slot)
+    for (; kt < nkf; ++kt) {
+      __builtin_amdgcn_sched_barrier(0);
+      step(0, kt, false, 0);
+      lin_wait_stage<C::kLPW, NS - 2>(nk - 2 - kt);
+      __builtin_amdgcn_sched_barrier(0);
+      step(1, kt + 1, false, 0);
+    }
   }
   if (nkf < nk) {
     // The part stage: chunks past the contraction hold copies; A's are made 0.
 #pragma unroll
-    for (int kk = 0; kk < 4; ++kk) {
-      if (2 * kk >= tail) break;
+    for (int kk = 0; kk < 2; ++kk) {
+      if (4 * kk >= tail) break;
       if (kk > 0)
 #pragma unroll
         for (int q = 0; q < NR; ++q) read_one(nkf, kk, q);
-      if (2 * kk + hl >= tail)
+      if (4 * kk + lc >= tail)
 #pragma unroll
-        for (int i = 0; i < TI; ++i) af[kk & 1][i] = i32x4{0, 0, 0, 0};
+        for (int i = 0; i < TI; ++i) af[kk][i] = i32x4{0, 0, 0, 0};
 #pragma unroll
       for (int t = 0; t < NP; ++t) product(kk, t);
     }
   }
   lin_wait_barrier<0>();
 
-  // Epilogue, 32 rows at a time: the scaled values go through LDS (a part of
+  // Epilogue, 16 rows at a time: the scaled values go through LDS (a part of
   // it per wave) so that residual, bias and output move in 16-byte runs of a row.
-  float* ost = reinterpret_cast<float*>(lin_smem) + w * 32 * C::kOutLd;
+  float* ost = reinterpret_cast<float*>(lin_smem) + w * 16 * C::kOutLd;
 #pragma unroll
   for (int i = 0; i < TI; ++i) {
-    const float rs = s_rs[wm * WM + 32 * i + l32];
+    const float rs = s_rs[wm * WM + 16 * i + lr];
 #pragma unroll
-    for (int j = 0; j < TJ; ++j)
+    for (int j = 0; j < TJ; ++j) {
+      const int cl = 16 * j + 4 * lc;                          // its four consecutive columns
+      const f32x4 c4 = *reinterpret_cast<const f32x4*>(&s_cs[wn * WN + cl]);
+      f32x4 o;
 #pragma unroll
-      for (int vq = 0; vq < 4; ++vq) {
-        const int cl = 32 * j + 8 * vq + 4 * hl;
-        const f32x4 c4 = *reinterpret_cast<const f32x4*>(&s_cs[wn * WN + cl]);
-        f32x4 o;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = mul_rn(mul_rn((float)acc[i][j][4 * vq + e], rs), c4[e]);
-        *reinterpret_cast<f32x4*>(ost + l32 * C::kOutLd + cl) = o;
-      }
+      for (int e = 0; e < 4; ++e) o[e] = mul_rn(mul_rn((float)acc[i][j][e], rs), c4[e]);
+      *reinterpret_cast<f32x4*>(ost + lr * C::kOutLd + cl) = o;
+    }
     asm volatile("" ::: "memory");     // one wave's LDS accesses stay in order; keep the compiler's too
     constexpr int CPR = WN / 8;
-    for (int t = lane; t < 32 * CPR; t += 64) {
+    for (int t = lane; t < 16 * CPR; t += 64) {
       const int row = t / CPR, c8 = 8 * (t % CPR);
-      const int64_t m = m0 + wm * WM + 32 * i + row;
+      const int64_t m = m0 + wm * WM + 16 * i + row;
       const int32_t n = n0 + wn * WN + c8;
       if (m >= p.M || n >= p.N) continue;
       float v[8];
@@ -456,11 +509,12 @@ static hipError_t launch_linear_tile(const LinearArgs& p, hipStream_t s) {
 // fixed + q (tile + nk stage) microseconds.  The three numbers of a form are
 // fitted to its measured times over 100 products (M 1 .. 8192, N 48 .. 32768,
 // K 128 .. 16384, operands from HBM); the form with the least estimate was on
-// average 1.4% and at most 24% slower than the best of 18 forms measured.  What
+// average 1.4% and at most 26% slower than the best of 18 forms measured.  What
 // they express: a unit takes in at most 55 to 60 bytes per ns while weights
 // come from HBM (95 if everything were in L2), so the stage times are those of
-// (BM + BN) 128 bytes except for the two largest tiles, which the products
-// bound; small tiles have the shorter ramp and epilogue.
+// (BM + BN) 128 bytes except for the largest tiles, which the products (and the
+// card's power: 1.6 GHz then) bound; small tiles have the shorter ramp and
+// epilogue.
 struct LinForm {
   int32_t bm, bn;
   double fixed, tile, stage;
@@ -468,18 +522,19 @@ struct LinForm {
   hipError_t (*launch)(const LinearArgs&, hipStream_t);
 };
 static const LinForm kLinForms[] = {
-    {16, 16, 1.499, 1.137, 0.050, 16, launch_linear_split<16, 16, 8, 2>},
-    {32, 16, 1.870, 0.717, 0.070, 32, launch_linear_split<32, 16, 8, 1>},
-    {32, 32, 1.100, 1.547, 0.089, 32, launch_linear_split<32, 32, 8, 1>},
-    {64, 16, 1.870, 1.069, 0.103, 2048, launch_linear_split<64, 16, 8, 1>},
-    {64, 32, 0.334, 2.804, 0.131, 2048, launch_linear_split<64, 32, 8, 1>},
-    {64, 64, 0.000, 4.123, 0.185, 2048, launch_linear_split<64, 64, 4, 2>},
-    {64, 64, 1.930, 1.665, 0.257, INT64_MAX, launch_linear_tile<64, 64, 32, 32, 4>},
-    {64, 128, 1.822, 2.218, 0.408, INT64_MAX, launch_linear_tile<64, 128, 32, 64, 3>},
-    {128, 128, 0.000, 4.531, 0.519, INT64_MAX, launch_linear_tile<128, 128, 64, 32, 4>},
-    {128, 256, 0.000, 5.414, 0.860, INT64_MAX, launch_linear_tile<128, 256, 64, 64, 3>},
-    {192, 256, 0.000, 6.006, 1.333, INT64_MAX, launch_linear_tile<192, 256, 96, 64, 2>},
-    {256, 256, 0.000, 6.823, 1.479, INT64_MAX, launch_linear_tile<256, 256, 128, 64, 2>},
+    {16, 16, 1.506, 1.135, 0.050, 16, launch_linear_split<16, 16, 8, 2>},
+    {32, 16, 1.875, 0.708, 0.069, 32, launch_linear_split<32, 16, 8, 1>},
+    {32, 32, 1.098, 1.538, 0.090, 32, launch_linear_split<32, 32, 8, 1>},
+    {64, 16, 1.866, 1.068, 0.103, 2048, launch_linear_split<64, 16, 8, 1>},
+    {64, 32, 0.307, 2.818, 0.131, 2048, launch_linear_split<64, 32, 8, 1>},
+    {64, 64, 0.000, 4.111, 0.185, 2048, launch_linear_split<64, 64, 4, 2>},
+    {64, 64, 2.675, 0.924, 0.270, INT64_MAX, launch_linear_tile<64, 64, 32, 32, 2>},
+    {128, 64, 2.230, 2.178, 0.409, INT64_MAX, launch_linear_tile<128, 64, 64, 32, 3>},
+    {128, 128, 0.000, 4.528, 0.467, INT64_MAX, launch_linear_tile<128, 128, 64, 32, 4>},
+    {128, 256, 0.000, 6.319, 0.869, INT64_MAX, launch_linear_tile<128, 256, 64, 64, 3>},
+    {160, 256, 0.000, 6.869, 1.023, INT64_MAX, launch_linear_tile<160, 256, 80, 64, 3>},
+    {192, 256, 0.000, 7.075, 1.151, INT64_MAX, launch_linear_tile<192, 256, 96, 64, 2>},
+    {256, 256, 0.000, 7.877, 1.385, INT64_MAX, launch_linear_tile<256, 256, 128, 64, 2>},
 };
 constexpr int64_t kLinUnits = 256;            // compute units
 constexpr int64_t kLinMaxTiles = 1 << 23;     // fewer than 2^32 threads of up to 512 per tile
