@@ -49,7 +49,12 @@ __device__ __forceinline__ void lin_wait_stage(int rem) {
 }
 
 // Eight outputs of row m from column n (below N), scaled: bias and residual added,
-// rounded once and stored, in 16-byte runs where the operands allow it.
+// rounded once and stored, in 16-byte runs where the operands allow it.  The
+// stores are non-temporal: all tiles of a round finish together, and their
+// outputs need not push the operands out of L2 (5632 x 28160 x 5120 716 -> 690
+// us, 2560 x 4096 x 4096 in 256 x 256 tiles 54.8 -> 44.0).  The residual's
+// reads are ordinary ones: it was written shortly before (2560 x 4096 x 4096
+// 41.2 us a pass, 43.7 past the caches).
 template <bool BF>
 __device__ __forceinline__ void lin_store(const LinearArgs& p, int64_t m, int32_t n, float* v) {
   using E = Elem16<BF>;
@@ -65,7 +70,7 @@ __device__ __forceinline__ void lin_store(const LinearArgs& p, int64_t m, int32_
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = add_rn(v[e], b[e]);
     }
-    *reinterpret_cast<i32x4*>(reinterpret_cast<uint16_t*>(p.y) + m * p.ldy + n) = E::pack(v);
+    __builtin_nontemporal_store(E::pack(v), reinterpret_cast<i32x4*>(reinterpret_cast<uint16_t*>(p.y) + m * p.ldy + n));
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -507,9 +512,9 @@ static hipError_t launch_linear_tile(const LinearArgs& p, hipStream_t s) {
 // The forms a product may take, and what each costs.  A compute unit takes
 // q = ceil(tiles / 256) tiles; a tile of nk 128-byte stages then costs about
 // fixed + q (tile + nk stage) microseconds.  The three numbers of a form are
-// fitted to its measured times over 100 products (M 1 .. 8192, N 48 .. 32768,
+// fitted to its measured times over 136 products (M 1 .. 8192, N 48 .. 32768,
 // K 128 .. 16384, operands from HBM); the form with the least estimate was on
-// average 1.4% and at most 26% slower than the best of 18 forms measured.  What
+// average 1.5% and at most 22% slower than the best of 16 forms measured.  What
 // they express: a unit takes in at most 55 to 60 bytes per ns while weights
 // come from HBM (95 if everything were in L2), so the stage times are those of
 // (BM + BN) 128 bytes except for the largest tiles, which the products (and the
@@ -522,19 +527,19 @@ struct LinForm {
   hipError_t (*launch)(const LinearArgs&, hipStream_t);
 };
 static const LinForm kLinForms[] = {
-    {16, 16, 1.506, 1.135, 0.050, 16, launch_linear_split<16, 16, 8, 2>},
-    {32, 16, 1.875, 0.708, 0.069, 32, launch_linear_split<32, 16, 8, 1>},
-    {32, 32, 1.098, 1.538, 0.090, 32, launch_linear_split<32, 32, 8, 1>},
-    {64, 16, 1.866, 1.068, 0.103, 2048, launch_linear_split<64, 16, 8, 1>},
-    {64, 32, 0.307, 2.818, 0.131, 2048, launch_linear_split<64, 32, 8, 1>},
-    {64, 64, 0.000, 4.111, 0.185, 2048, launch_linear_split<64, 64, 4, 2>},
-    {64, 64, 2.675, 0.924, 0.270, INT64_MAX, launch_linear_tile<64, 64, 32, 32, 2>},
-    {128, 64, 2.230, 2.178, 0.409, INT64_MAX, launch_linear_tile<128, 64, 64, 32, 3>},
-    {128, 128, 0.000, 4.528, 0.467, INT64_MAX, launch_linear_tile<128, 128, 64, 32, 4>},
-    {128, 256, 0.000, 6.319, 0.869, INT64_MAX, launch_linear_tile<128, 256, 64, 64, 3>},
-    {160, 256, 0.000, 6.869, 1.023, INT64_MAX, launch_linear_tile<160, 256, 80, 64, 3>},
-    {192, 256, 0.000, 7.075, 1.151, INT64_MAX, launch_linear_tile<192, 256, 96, 64, 2>},
-    {256, 256, 0.000, 7.877, 1.385, INT64_MAX, launch_linear_tile<256, 256, 128, 64, 2>},
+    {16, 16, 1.429, 1.141, 0.049, 16, launch_linear_split<16, 16, 8, 2>},
+    {32, 16, 1.798, 0.712, 0.070, 32, launch_linear_split<32, 16, 8, 1>},
+    {32, 32, 1.002, 1.506, 0.094, 32, launch_linear_split<32, 32, 8, 1>},
+    {64, 16, 1.633, 1.167, 0.109, 2048, launch_linear_split<64, 16, 8, 1>},
+    {64, 32, 0.101, 2.871, 0.139, 2048, launch_linear_split<64, 32, 8, 1>},
+    {64, 64, 0.000, 4.096, 0.194, 2048, launch_linear_split<64, 64, 4, 2>},
+    {64, 64, 2.288, 1.328, 0.272, INT64_MAX, launch_linear_tile<64, 64, 32, 32, 2>},
+    {128, 64, 1.217, 3.279, 0.409, INT64_MAX, launch_linear_tile<128, 64, 64, 32, 3>},
+    {128, 128, 0.000, 5.054, 0.481, INT64_MAX, launch_linear_tile<128, 128, 64, 32, 4>},
+    {128, 256, 0.000, 7.064, 0.892, INT64_MAX, launch_linear_tile<128, 256, 64, 64, 3>},
+    {160, 256, 0.000, 7.853, 1.043, INT64_MAX, launch_linear_tile<160, 256, 80, 64, 3>},
+    {192, 256, 0.000, 8.138, 1.171, INT64_MAX, launch_linear_tile<192, 256, 96, 64, 2>},
+    {256, 256, 0.000, 10.317, 1.376, INT64_MAX, launch_linear_tile<256, 256, 128, 64, 2>},
 };
 constexpr int64_t kLinUnits = 256;            // compute units
 constexpr int64_t kLinMaxTiles = 1 << 23;     // fewer than 2^32 threads of up to 512 per tile

@@ -9,7 +9,8 @@
 // element for some ten operations.  A workgroup holds one row in registers
 // (a thread the 8-element chunks tid, tid + T, ...), so every element is read
 // and written once; the row's sum of squares and largest |y| go round its waves
-// (through LDS if there are several).
+// (through LDS if there are several).  Rows of h and y leave non-temporally: no
+// workgroup reads them again (1337 x 3584 norms 10.5 -> 9.3 us).
 #include "common.h"
 #include "elem16.h"
 #include "launch.h"
@@ -125,7 +126,8 @@ rmsnorm_quantize_kernel(NormArgs a) {
       E::unpack(hv[i], f);
     }
     if (a.h && tid + NT * i < nch)
-      *reinterpret_cast<i32x4*>(reinterpret_cast<uint16_t*>(a.h) + m * a.ldh + 8 * (tid + NT * i)) = hv[i];
+      __builtin_nontemporal_store(
+          hv[i], reinterpret_cast<i32x4*>(reinterpret_cast<uint16_t*>(a.h) + m * a.ldh + 8 * (tid + NT * i)));
 #pragma unroll
     for (int e = 0; e < 8; ++e) ss = fma((double)f[e], (double)f[e], ss);
     __builtin_amdgcn_sched_barrier(0);
@@ -150,7 +152,9 @@ rmsnorm_quantize_kernel(NormArgs a) {
 #pragma unroll
     for (int i = 0; i < MAXC; ++i) {
       const int c = tid + NT * i;
-      if (c < nch) *reinterpret_cast<i32x4*>(reinterpret_cast<uint16_t*>(a.y) + m * a.ldy + 8 * c) = E::pack(y[i]);
+      if (c < nch)
+        __builtin_nontemporal_store(E::pack(y[i]),
+                                    reinterpret_cast<i32x4*>(reinterpret_cast<uint16_t*>(a.y) + m * a.ldy + 8 * c));
     }
   if (!a.xq) return;
   const float qm = (float)((1 << (a.bits - 1)) - 1);
@@ -228,7 +232,7 @@ silu_mul_quantize_kernel(GateArgs a) {
 // that eight waves per SIMD leave, and waves beyond the row's chunks would
 // only repeat its reductions: 2560 x 11264 gates take 28.9 us (5.0 TB/s, where
 // a large copy runs at 5.1) at two chunks with the row's own eleven waves, 31.4
-// with sixteen, 30.9 at four chunks; 5632 x 5120 norms 41.3 (4.9 TB/s), 44.6
+// with sixteen, 30.9 at four chunks; 5632 x 5120 norms 40.3 (5.0 TB/s), 44.6
 // with eight waves for five, 50.6 at one chunk.  Rows of one wave take one chunk
 // (8192 x 256 norms 6.5 us, 7.8 at two); rows past 16 waves of two take four or
 // eight (512 x 32768 gates 19.8 us, 100 x 65536 norms 25.3).

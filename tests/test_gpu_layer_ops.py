@@ -320,6 +320,26 @@ LINEAR = [(1, 1, 16), (1, 256, 256), (2, 17, 48), (5, 100, 112), (15, 1000, 1008
           (255, 24, 2048), (257, 513, 208), (333, 1001, 1008), (640, 1300, 528), (1000, 9, 4112), (2100, 2052, 160)]
 
 
+# Ragged products of one part stage, a part second one, three and four whole
+# ones, and five with a part, in sizes that give every form of the product.
+FORMS = [(1, 65, 384), (1, 65, 1008), (17, 65, 208), (17, 65, 656), (1, 4105, 96), (1, 4101, 208), (1, 4097, 384),
+         (1, 4107, 1008), (33, 65, 96), (34, 65, 512), (65, 2057, 96), (33, 4145, 384), (33, 8387, 1008), (1, 8209, 96),
+         (1, 8193, 208), (1, 8215, 384), (1, 8199, 512), (2099, 65, 656), (66, 8613, 96), (66, 8293, 208),
+         (65, 8365, 384), (66, 8201, 512), (67, 8297, 656), (66, 16621, 96), (1, 16433, 208), (33, 17121, 384),
+         (33, 16595, 512), (33, 16831, 656), (131, 16991, 96), (132, 16397, 208), (130, 16845, 384), (131, 16463, 512),
+         (130, 16753, 656), (394, 16721, 96), (390, 16667, 208), (397, 16531, 384), (395, 16589, 512),
+         (388, 16729, 656), (484, 16591, 96), (491, 16693, 208), (490, 16825, 384), (484, 16945, 512),
+         (485, 16499, 656), (577, 17197, 96), (585, 16567, 208), (587, 16661, 384), (591, 16387, 512), (577, 17089, 432)]
+
+
+@pytest.mark.parametrize("M,N,K", FORMS)
+def test_linear_forms(M, N, K):
+    dt = BF16 if (M + K // 16) % 2 else F16
+    xq, sx, wq, sw, bias, res = linear_inputs(M + 3 * N + 5 * K, M, N, K, dt == BF16, full=True)
+    got = run_linear(xq, sx, wq, sw, dt, bias, res)
+    assert np.array_equal(got, L.linear_i8(xq, sx, wq, sw, bias, res, dt == BF16))
+
+
 @pytest.mark.parametrize("dt", [F16, BF16], ids=["f16", "bf16"])
 @pytest.mark.parametrize("M,N,K", LINEAR)
 def test_linear_matches_definition(M, N, K, dt):
