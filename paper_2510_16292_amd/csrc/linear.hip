@@ -11,6 +11,8 @@
 // (32x32x32 products have the same rate and half the instructions, but cost
 // more power, which is what bounds a long product: 8192^3 449 us with them,
 // 418 with these.)
+#include <math.h>
+
 #include "common.h"
 #include "elem16.h"
 #include "launch.h"
@@ -342,6 +344,15 @@ linear_tile_kernel(LinearArgs p, int32_t tiles_n, int32_t gm) {
 // chunk l / 16 of its operand; output: column 4 (l / 16) + v of the first
 // operand's rows, row l % 16 of the second's).
 // ---------------------------------------------------------------------------
+// Tile rows that xcd_tile walks together: as xcd_group_rows chooses them (the
+// fewest operand rows in an XCD's share, or among the 32 tiles it runs at once
+// where the share is many times that), without its search over the tile rows.
+static int lin_group_rows(int64_t tiles_m, int64_t tiles_n) {
+  const double share = (double)(tiles_m * tiles_n) / 8;
+  const double g = share > 128 && tiles_n >= 6 ? 5.0 : sqrt(share);
+  return (int)(g < 1.0 ? 1.0 : g > (double)tiles_m ? (double)tiles_m : g + 0.5);
+}
+
 template <int N>
 __device__ __forceinline__ void lin_wait_loads() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
@@ -489,7 +500,7 @@ static hipError_t launch_linear_split(const LinearArgs& p, hipStream_t s) {
   const int tn = (p.N + BN - 1) / BN;
   const int64_t tm = (p.M + BM - 1) / BM;
   KernelScope ks("linear_i8_split", s);
-  QSVD_LAUNCH(ks, kern, dim3((unsigned)(tm * tn)), dim3(C::kThreads), C::kLds, s, p, tn, xcd_group_rows(tm, tn, 32));
+  QSVD_LAUNCH(ks, kern, dim3((unsigned)(tm * tn)), dim3(C::kThreads), C::kLds, s, p, tn, lin_group_rows(tm, tn));
   return hipGetLastError();
 }
 
@@ -505,7 +516,7 @@ static hipError_t launch_linear_tile(const LinearArgs& p, hipStream_t s) {
   const int tn = (p.N + BN - 1) / BN;
   const int64_t tm = (p.M + BM - 1) / BM;
   KernelScope ks("linear_i8_tile", s);
-  QSVD_LAUNCH(ks, kern, dim3((unsigned)(tm * tn)), dim3(C::kThreads), C::kLds, s, p, tn, xcd_group_rows(tm, tn, 32));
+  QSVD_LAUNCH(ks, kern, dim3((unsigned)(tm * tn)), dim3(C::kThreads), C::kLds, s, p, tn, lin_group_rows(tm, tn));
   return hipGetLastError();
 }
 

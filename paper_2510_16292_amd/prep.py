@@ -173,6 +173,15 @@ def quantize_layer(A: np.ndarray, B: np.ndarray, n_q_heads: int, n_kv_heads: int
                          np.ascontiguousarray(a_codes), s_a, np.ascontiguousarray(b_codes), s_b)
 
 
+def quantize_linear(W: np.ndarray, clip: float = 1.0):
+    """Weight of one W8A8 linear layer Y = X W (K x N) for qsvd_linear_i8: int8
+    codes [N][K] and fp32 scales [N], one per output channel."""
+    K, _ = W.shape
+    assert K % 16 == 0, "the contraction of a W8A8 product is a multiple of 16"
+    codes, scale = _quantize_t(np.ascontiguousarray(np.asarray(W, dtype=np.float64).T), 8, 0, clip)
+    return np.ascontiguousarray(codes), scale
+
+
 def prepare_from_weight(W, r, n_q_heads, n_kv_heads, head_dim, beta=0.5, w_bits=8, w_group=0, clip=1.0):
     A, B = truncated_factors(W, r, beta)
     return quantize_layer(A, B, n_q_heads, n_kv_heads, head_dim, w_bits, w_group, clip)

@@ -121,3 +121,17 @@ def test_linear_by_hand():
     out = L.linear_i8(xq, [0.5, 1.0], wq, [2.0, 0.25], [1.0, 0.0], np.array([[0.0, 8.0], [0.0, 0.0]]), False)
     # 127 * 15 * 2 + 1 = 3811 and -127^2 * 3 / 4 = -12096.75 as fp16 (steps of 2, ties to even, and of 8)
     assert out.tolist() == [[13.0, -254 * 0.125 + 8.0], [3812.0, -12096.0]]
+
+
+def test_quantize_linear_layout():
+    """prep.quantize_linear: codes [N][K] and a scale per output channel, off by
+    at most half a step."""
+    from paper_2510_16292_amd import prep
+    W = np.random.default_rng(0).standard_normal((32, 5))
+    W[:, 3] = 0
+    codes, scale = prep.quantize_linear(W)
+    assert codes.shape == (5, 32) and codes.dtype == np.int8 and scale.shape == (5,) and scale.dtype == np.float32
+    assert scale[3] == 1 and not codes[3].any()
+    assert np.all(np.abs(codes.T * scale.astype(np.float64) - W) <= scale / 2 * (1 + 1e-6))
+    with pytest.raises(AssertionError):
+        prep.quantize_linear(W[:24])
