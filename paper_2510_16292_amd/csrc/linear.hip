@@ -554,19 +554,79 @@ static const LinForm kLinForms[] = {
 };
 constexpr int64_t kLinUnits = 256;            // compute units
 constexpr int64_t kLinMaxTiles = 1 << 23;     // fewer than 2^32 threads of up to 512 per tile
+constexpr double kLinTwoFrom = 40.0;          // us of a product that may be made in two,
+constexpr int32_t kLinTwoK = 1024;            // its least contraction,
+constexpr double kLinTwoGain = 0.98;          // what it must come to
+constexpr double kLinTwoCost = 2.0;           // with a second launch
+
+struct LinChoice {
+  const LinForm* form;      // NULL: none
+  double us;
+};
+static int64_t lin_tiles(int64_t n, int32_t b) { return (n + b - 1) / b; }
+
+static LinChoice lin_choose(int64_t M, int32_t N, int32_t K) {
+  LinChoice best{nullptr, 0.0};
+  const double nk = (double)lin_tiles(K, kLinStage);
+  for (const LinForm& f : kLinForms) {
+    const int64_t tiles = lin_tiles(M, f.bm) * lin_tiles(N, f.bn);
+    if (M > f.max_m || tiles >= kLinMaxTiles) continue;
+    const double us = f.fixed + (double)lin_tiles(tiles, kLinUnits) * (f.tile + nk * f.stage);
+    if (!best.form || us < best.us) best = LinChoice{&f, us};
+  }
+  return best;
+}
 
 hipError_t launch_linear_i8(const LinearArgs& p, hipStream_t s) {
   if (p.M == 0) return hipSuccess;
-  const LinForm* best = nullptr;
-  double least = 0.0;
-  const double nk = (double)((p.K + kLinStage - 1) / kLinStage);
-  for (const LinForm& f : kLinForms) {
-    const int64_t tiles = ((p.M + f.bm - 1) / f.bm) * (((int64_t)p.N + f.bn - 1) / f.bn);
-    if (p.M > f.max_m || tiles >= kLinMaxTiles) continue;
-    const double q = (double)((tiles + kLinUnits - 1) / kLinUnits), us = f.fixed + q * (f.tile + nk * f.stage);
-    if (!best || us < least) best = &f, least = us;
+  LinChoice one = lin_choose(p.M, p.N, p.K);
+  if (!one.form) return hipErrorInvalidConfiguration;
+  // A long product whose tiles leave most units idle in their last round is
+  // made in two: whole rounds of one form over the first columns or rows, and
+  // what is left in the form (or two) that suits it: 5632 x 28160 x 5120 in 8.9
+  // rounds of 256 x 256 tiles and one of 160 x 256, 608 us, in 9.5 rounds 678;
+  // 6033 x 2617 x 12176 228 us for 306.  Over 84 random products from 40 us on
+  // 2.8% on average (one in two 13% slower, three 3%); short contractions, whose
+  // stores the estimate does not see, were up to 9% slower and stay in one.
+  int32_t n1 = p.N;
+  int64_t m1 = p.M;
+  if (one.us > kLinTwoFrom && p.K >= kLinTwoK) {
+    double least = kLinTwoGain * one.us - kLinTwoCost;
+    const double nk = (double)lin_tiles(p.K, kLinStage);
+    const LinForm* first = nullptr;
+    for (const LinForm& f : kLinForms) {
+      const int64_t tm = lin_tiles(p.M, f.bm), tn = lin_tiles(p.N, f.bn), rounds = lin_tiles(tm * tn, kLinUnits) - 1;
+      if (p.M > f.max_m || tm * tn >= kLinMaxTiles || rounds < 1) continue;
+      const double us = f.fixed + (double)rounds * (f.tile + nk * f.stage);
+      const int64_t cols = rounds * kLinUnits / tm * f.bn, rws = rounds * kLinUnits / tn * f.bm;
+      for (int by_rows = 0; by_rows < 2; ++by_rows) {
+        if (by_rows ? rws < 1 || rws >= p.M : cols < 1 || cols >= p.N) continue;
+        const LinChoice rest = by_rows ? lin_choose(p.M - rws, p.N, p.K) : lin_choose(p.M, (int32_t)(p.N - cols), p.K);
+        if (!rest.form || us + rest.us >= least) continue;
+        least = us + rest.us;
+        first = &f;
+        m1 = by_rows ? rws : p.M;
+        n1 = by_rows ? p.N : (int32_t)cols;
+      }
+    }
+    if (first) one.form = first;
   }
-  return best ? best->launch(p, s) : hipErrorInvalidConfiguration;
+  LinearArgs a = p;
+  a.M = m1;
+  a.N = n1;
+  if (hipError_t e = one.form->launch(a, s); e != hipSuccess || (m1 == p.M && n1 == p.N)) return e;
+  const int64_t m0 = m1 < p.M ? m1 : 0;
+  const int32_t n0 = n1 < p.N ? n1 : 0;
+  a.M = p.M - m0;
+  a.N = p.N - n0;
+  a.x = p.x + m0 * p.ldx;
+  a.sx = p.sx + m0;
+  a.w = p.w + (int64_t)n0 * p.K;
+  a.sw = p.sw + n0;
+  if (p.bias) a.bias = (const uint16_t*)p.bias + n0;
+  if (p.residual) a.residual = (const uint16_t*)p.residual + m0 * p.ldr + n0;
+  a.y = (uint16_t*)p.y + m0 * p.ldy + n0;
+  return launch_linear_i8(a, s);
 }
 
 }  // namespace qsvd

@@ -340,6 +340,16 @@ def test_linear_forms(M, N, K):
     assert np.array_equal(got, L.linear_i8(xq, sx, wq, sw, bias, res, dt == BF16))
 
 
+@pytest.mark.parametrize("M,N,K,ldy", [(33, 17179, 10896, 17184), (131, 6019, 11744, 6019), (5456, 141, 11952, 144),
+                                       (342, 3130, 12736, 3136), (1907, 2611, 4112, 2612)])
+def test_linear_in_two_parts(M, N, K, ldy):
+    """Long products whose last round would be nearly idle: columns or rows in two
+    launches, with bias, residual and strides."""
+    xq, sx, wq, sw, bias, res = linear_inputs(M + N + K, M, N, K, True, full=True)
+    got = run_linear(xq, sx, wq, sw, BF16, bias, res, ldx=K + 32, ldy=ldy)
+    assert np.array_equal(got, L.linear_i8(xq, sx, wq, sw, bias, res, True))
+
+
 @pytest.mark.parametrize("dt", [F16, BF16], ids=["f16", "bf16"])
 @pytest.mark.parametrize("M,N,K", LINEAR)
 def test_linear_matches_definition(M, N, K, dt):
