@@ -370,7 +370,8 @@ qsvd_status qsvd_rmsnorm_quantize_act(const void* x, int64_t ldx, const void* re
  *   sx        device fp32 [M]
  * exp, the quotient and the product are evaluated in fp32 to a few units in the
  * last place, so a code may differ by one from that of the exact y next to a
- * rounding border.  Tiny rows, values that are not finite and requirements as
+ * rounding border; an exp(-gate) past fp32 (a gate below -88.7) makes y 0.
+ * Tiny rows, values that are not finite and requirements as
  * for qsvd_rmsnorm_quantize_act. */
 qsvd_status qsvd_silu_mul_quantize_act(const void* gate, int64_t ldg, const void* up, int64_t ldu, int64_t M,
                                        int32_t K, int32_t dtype, int32_t bits, float clip, void* xq, float* sx,

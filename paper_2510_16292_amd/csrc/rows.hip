@@ -172,14 +172,16 @@ rmsnorm_quantize_kernel(NormArgs a) {
 // silu(g) = g / (1 + e^-g).  e^-g as 2^p with p = -g log2(e) in two parts: the
 // hardware's 2^p of the rounded p, times 1 + (what rounding p left out) ln 2;
 // an e^-g past fp32 is inf and makes the quotient 0.  Past +-200 e^-g is 0 or
-// inf already, so g is held there (p and its remainder stay finite).
+// inf already, so g is held there (p and its remainder stay finite).  Both
+// sides of the quotient are quarters: the hardware's reciprocal gives 0 for
+// results below the normal numbers, which those of e^-g > 2^126 would be.
 __device__ __forceinline__ float silu(float g) {
   const float kHi = 1.44269502f, kLo = 1.92596303e-8f, kLn2 = 0.693147181f;
   const float t = __builtin_amdgcn_fmed3f(g, -200.f, 200.f);
   const float p = -t * kHi;
   const float lo = fmaf(-t, kLo, fmaf(-t, kHi, -p));
   const float ex = __builtin_amdgcn_exp2f(p) * fmaf(lo, kLn2, 1.f);
-  return g * __builtin_amdgcn_rcpf(1.f + ex);
+  return 0.25f * g * __builtin_amdgcn_rcpf(fmaf(0.25f, ex, 0.25f));
 }
 
 template <bool BF, int MAXC>

@@ -272,6 +272,20 @@ def test_gate_special_rows(dt):
         assert np.isnan(s[i]) and not q[i].any()
 
 
+@pytest.mark.parametrize("dt", [F16, BF16], ids=["f16", "bf16"])
+def test_gate_next_to_the_largest_exponential(dt):
+    """Gates whose e^-g is within fp32 but has a reciprocal below its normal
+    numbers: the product with up is normal, and so are the codes."""
+    bf = dt == BF16
+    K = 136
+    g = np.random.default_rng(18)
+    gate = L.round16(np.linspace(-88.5, -87.5, 3 * K).reshape(3, K), bf)
+    up = L.round16(g.uniform(100, 1000, (3, K)), bf)
+    q, s = run_gate(gate, up, dt)
+    assert np.abs(q).max(axis=1).tolist() == [127] * 3
+    check_gate((q, s), gate, up)
+
+
 # ---------------------------------------------------------------- linear
 
 def run_linear(xq, sx, wq, sw, dt, bias=None, res=None, ldx=None, ldy=None, offset=0, alias=False):
