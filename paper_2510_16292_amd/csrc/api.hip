@@ -554,9 +554,9 @@ constexpr int32_t kMaxRowK = 65536;
 // tiles of at least 64 x 64 outputs of up to 512.
 constexpr int64_t kMaxRows = ((int64_t)1 << 22) - 1;
 constexpr int64_t kMaxTiles = ((int64_t)1 << 23) - 1;
-// Contraction of a W8A8 product whose sum of int8 products fits an int32:
-// 131072 * 128 * 127 < 2^31.
-constexpr int32_t kMaxLinearK = 131072;
+// Longest contraction of a W8A8 product: 131072 products of -128 and -128 are
+// 2^31, one too many for its int32 sum.
+constexpr int32_t kMaxLinearK = 131072 - 16;
 // Widest row stride of codes: a tile's 256 row offsets fit 31 bits.
 constexpr int64_t kMaxLinearLd = (int64_t)1 << 22;
 
@@ -600,7 +600,10 @@ qsvd_status qsvd_rmsnorm_quantize_act(const void* x, int64_t ldx, const void* re
       {"x", x, ldx}, {"residual", residual, ldr}, {"h", h, ldh}, {"y", y, ldy}};
   for (const auto& r : rows)
     if ((st = check_row_operand(r.name, r.p, r.ld, K)) != QSVD_OK) return st;
-  if (!aligned(gamma, 16) || !aligned(xq, 8)) return fail(QSVD_ERR_UNSUPPORTED, "gamma must be 16-byte and xq 8-byte aligned");
+  if (!aligned(gamma, 16) || !aligned(xq, 8) || !aligned(sx, 4))
+    return fail(QSVD_ERR_UNSUPPORTED, "gamma must be 16-byte, xq 8-byte and sx 4-byte aligned");
+  if (h && M > 1 && ((h == x && ldh != ldx) || (h == residual && ldh != ldr)))
+    return fail(QSVD_ERR_INVALID_ARG, "h in place of x or residual must have its row stride");
   const NormArgs a{x, ldx, residual, ldr, gamma, M, K, dtype, eps, bits, clip, h, ldh, y, ldy, xq, sx};
   return hip_status(launch_rmsnorm_quantize(a, (hipStream_t)stream), "rmsnorm_quantize_act");
 }
@@ -613,7 +616,7 @@ qsvd_status qsvd_silu_mul_quantize_act(const void* gate, int64_t ldg, const void
   if (!gate || !up || !xq || !sx) return fail(QSVD_ERR_INVALID_ARG, "NULL pointer");
   if ((st = check_row_operand("gate", gate, ldg, K)) != QSVD_OK) return st;
   if ((st = check_row_operand("up", up, ldu, K)) != QSVD_OK) return st;
-  if (!aligned(xq, 8)) return fail(QSVD_ERR_UNSUPPORTED, "xq must be 8-byte aligned");
+  if (!aligned(xq, 8) || !aligned(sx, 4)) return fail(QSVD_ERR_UNSUPPORTED, "xq must be 8-byte and sx 4-byte aligned");
   const GateArgs a{gate, ldg, up, ldu, M, K, dtype, bits, clip, xq, sx};
   return hip_status(launch_silu_mul_quantize(a, (hipStream_t)stream), "silu_mul_quantize_act");
 }
@@ -633,8 +636,10 @@ qsvd_status qsvd_linear_i8(const void* xq, int64_t ldx, const float* sx, const v
   if (K > kMaxLinearK) return fail(QSVD_ERR_UNSUPPORTED, "K must be at most %d", kMaxLinearK);
   if (ldx > kMaxLinearLd) return fail(QSVD_ERR_UNSUPPORTED, "the row stride of xq must be at most %lld", (long long)kMaxLinearLd);
   if (!aligned(xq, 16) || !aligned(wq, 16)) return fail(QSVD_ERR_UNSUPPORTED, "xq and wq must be 16-byte aligned");
-  if (!aligned(y, 2) || !aligned(residual, 2) || !aligned(bias, 2))
-    return fail(QSVD_ERR_UNSUPPORTED, "y, residual and bias must be aligned to their elements");
+  if (!aligned(y, 2) || !aligned(residual, 2) || !aligned(bias, 2) || !aligned(sx, 4) || !aligned(sw, 4))
+    return fail(QSVD_ERR_UNSUPPORTED, "y, residual, bias, sx and sw must be aligned to their elements");
+  if (y == residual && ldy != ldr && M > 1)
+    return fail(QSVD_ERR_INVALID_ARG, "y in place of residual must have its row stride");
   if (M / 64 + 1 > kMaxTiles / (((int64_t)N + 63) / 64))
     return fail(QSVD_ERR_UNSUPPORTED, "(M / 64 + 1) * ceil(N / 64) must be below 2^23");
   const bool vec = ldy % 8 == 0 && aligned(y, 16) && (!residual || (ldr % 8 == 0 && aligned(residual, 16))) &&

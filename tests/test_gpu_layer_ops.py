@@ -364,6 +364,35 @@ def test_linear_in_two_parts(M, N, K, ldy):
     assert np.array_equal(got, L.linear_i8(xq, sx, wq, sw, bias, res, True))
 
 
+@pytest.mark.parametrize("M,N,K", [(131, 6019, 11744), (5456, 141, 11952)])
+def test_linear_in_two_parts_captured_in_place(M, N, K):
+    """The same, adding into its residual, captured once and replayed: a replay
+    adds the product again, as an eager call does."""
+    t = H.torch()
+    xq, sx, wq, sw, bias, res = linear_inputs(M + N + K, M, N, K, True, full=True)
+    xd, wd, sxd, swd = H.dev(xq), H.dev(wq), H.dev(sx.astype(np.float32)), H.dev(sw.astype(np.float32))
+    bd, y = up16(bias[None], BF16), up16(res, BF16)
+
+    def run():
+        B.check(B.qsvd_linear_i8(xd.data_ptr(), K, sxd.data_ptr(), wd.data_ptr(), swd.data_ptr(), M, N, K, bd.data_ptr(),
+                                 y.data_ptr(), N, BF16, y.data_ptr(), N, B.stream_handle()))
+
+    run()
+    want = L.linear_i8(xq, sx, wq, sw, bias, res, True)
+    assert np.array_equal(down16(y), want)
+    cg = t.cuda.CUDAGraph()
+    with t.cuda.graph(cg):
+        run()
+    for i in range(4):
+        y.copy_(up16(want, BF16))
+        want = L.linear_i8(xq, sx, wq, sw, bias, want, True)
+        if i % 2:
+            run()
+        else:
+            cg.replay()
+        assert np.array_equal(down16(y), want), i
+
+
 @pytest.mark.parametrize("dt", [F16, BF16], ids=["f16", "bf16"])
 @pytest.mark.parametrize("M,N,K", LINEAR)
 def test_linear_matches_definition(M, N, K, dt):
@@ -386,14 +415,14 @@ def test_linear_strides_and_alignment(M, N, K, ldx, ldy, offset):
 
 @pytest.mark.parametrize("M", [1, 32, 70, 300])
 def test_linear_longest_contraction(M):
-    """Every product 127 * 127 over the longest contraction: 131072 * 16129 is
-    below 2^31, partial sums as well."""
-    K, N = 131072, 40
-    xq = np.full((M, K), 127, np.int8)
-    wq = np.full((N, K), 127, np.int8)
-    wq[1::2] = -127
+    """Every product (-128) (-128) or (-128) 127 over the longest contraction:
+    131056 * 16384 is below 2^31, partial sums as well."""
+    K, N = 131056, 40
+    xq = np.full((M, K), -128, np.int8)
+    wq = np.full((N, K), -128, np.int8)
+    wq[1::2] = 127
     sx, sw = np.full(M, 2.0 ** -20, np.float32), np.full(N, 2.0 ** -4, np.float32)
-    acc = 127.0 * 127 * K * np.where(np.arange(N) % 2, -1, 1)
+    acc = -128.0 * K * np.where(np.arange(N) % 2, 127, -128)
     want = L.round16(np.broadcast_to(acc * 2.0 ** -24, (M, N)).astype(np.float32), True)
     assert np.array_equal(run_linear(xq, sx, wq, sw, BF16), want)
 

@@ -30,7 +30,8 @@ def norm(**kw):
     (dict(ldy=56), INV), (dict(K=60), UNS), (dict(K=65544, ldx=65544, ldr=65544, ldh=65544, ldy=65544), UNS),
     (dict(M=1 << 22), UNS), (dict(ldx=68), UNS), (dict(ldr=68), UNS), (dict(ldh=68), UNS), (dict(ldy=68), UNS),
     (dict(x=FAKE + 8), UNS), (dict(residual=FAKE + 8), UNS), (dict(gamma=FAKE + 8), UNS), (dict(h=FAKE + 8), UNS),
-    (dict(y=FAKE + 8), UNS), (dict(xq=FAKE + 4), UNS),
+    (dict(y=FAKE + 8), UNS), (dict(xq=FAKE + 4), UNS), (dict(sx=FAKE + 2), UNS),
+    (dict(ldx=72, residual=FAKE + 4096), INV), (dict(ldr=72, x=FAKE + 4096), INV),
     (dict(M=0), OK), (dict(M=0, x=0, gamma=0, y=0, xq=0, sx=0), OK),
 ])
 def test_norm_validation(kw, status):
@@ -50,7 +51,7 @@ def gate(**kw):
     (dict(gate=0), INV), (dict(up=0), INV), (dict(xq=0), INV), (dict(sx=0), INV), (dict(ldg=56), INV),
     (dict(ldu=56), INV), (dict(K=4), UNS), (dict(K=65544, ldg=65544, ldu=65544), UNS), (dict(M=1 << 22), UNS),
     (dict(ldg=68), UNS), (dict(ldu=68), UNS), (dict(gate=FAKE + 2), UNS), (dict(up=FAKE + 2), UNS),
-    (dict(xq=FAKE + 2), UNS), (dict(M=0), OK),
+    (dict(xq=FAKE + 2), UNS), (dict(sx=FAKE + 2), UNS), (dict(M=0), OK),
 ])
 def test_gate_validation(kw, status):
     assert gate(**kw) == status
@@ -69,7 +70,7 @@ def linear(**kw):
     (dict(M=-1), INV), (dict(N=0), INV), (dict(K=0), INV), (dict(dtype=7), INV), (dict(ldx=48), INV),
     (dict(ldy=23), INV), (dict(ldr=23), INV), (dict(xq=0), INV), (dict(sx=0), INV), (dict(wq=0), INV),
     (dict(sw=0), INV), (dict(y=0), INV), (dict(K=56), UNS), (dict(ldx=72), UNS),
-    (dict(K=131088, ldx=131088), UNS), (dict(ldx=(1 << 22) + 16), UNS), (dict(xq=FAKE + 8), UNS),
+    (dict(K=131072, ldx=131072), UNS), (dict(sx=FAKE + 2), UNS), (dict(sw=FAKE + 1), UNS), (dict(ldr=32), INV), (dict(ldx=(1 << 22) + 16), UNS), (dict(xq=FAKE + 8), UNS),
     (dict(wq=FAKE + 8), UNS), (dict(y=FAKE + 1), UNS), (dict(residual=FAKE + 1), UNS), (dict(bias=FAKE + 1), UNS),
     (dict(M=1 << 31, N=1 << 14, ldy=1 << 14, ldr=1 << 14), UNS), (dict(M=(1 << 63) - 1), UNS),
     (dict(M=0), OK), (dict(M=0, xq=0, y=0), OK),
