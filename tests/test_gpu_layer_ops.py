@@ -196,6 +196,33 @@ def test_norm_then_quantizer_of_the_library():
     assert np.array_equal(xq.view(np.int8), got["q"]) and np.array_equal(sx, got["s"])
 
 
+SHORT = [(1000, 64), (37, 128), (515, 256), (33, 40), (7, 24), (16, 248), (129, 200), (9, 264)]
+
+
+@pytest.mark.parametrize("M,K", SHORT)
+def test_short_rows(M, K):
+    """Rows that share a wave: counts that leave one part empty, rows that are not
+    finite and zero rows next to others, each output alone."""
+    g = np.random.default_rng(M + K)
+    for dt in (F16, BF16):
+        bf = dt == BF16
+        x, res, up = (rows16(g, M, K, bf) for _ in range(3))
+        gamma = L.round16(1 + 0.3 * g.standard_normal(K), bf)
+        for i, v in ((1, np.nan), (3, np.inf), (M - 2, -np.inf)):
+            x[i, (5 * i) % K] = v
+        x[4], res[4] = 0, 0
+        for want in (("h", "y", "q"), ("q",), ("y",)):
+            check_norm(run_norm(x, res, gamma, dt, want=want, pad=8), x, res, gamma, dt)
+        check_norm(run_norm(x, res, gamma, dt, bits=4, clip=0.8, alias="residual"), x, res, gamma, dt, bits=4, clip=0.8)
+        x[3], x[M - 2] = res[3], res[M - 2]             # (silu of -inf: NaN)
+        x = L.round16(np.clip(x, -20, 20), bf)
+        x[3, 0] = up[5, K - 1] = np.inf
+        q, s = run_gate(x, up, dt, pad=8)
+        bad = ~np.isfinite(x).all(axis=1) | ~np.isfinite(up).all(axis=1)
+        assert bad.sum() == 3 and np.isnan(s[bad]).all() and not q[bad].any()
+        check_gate((q[~bad], s[~bad]), x[~bad], up[~bad])
+
+
 # ---------------------------------------------------------------- gate
 
 def run_gate(gate, up, dt, bits=8, clip=1.0, halves=True, pad=0):
