@@ -642,9 +642,8 @@ qsvd_status qsvd_linear_i8(const void* xq, int64_t ldx, const float* sx, const v
     return fail(QSVD_ERR_INVALID_ARG, "y in place of residual must have its row stride");
   if (M / 64 + 1 > kMaxTiles / (((int64_t)N + 63) / 64))
     return fail(QSVD_ERR_UNSUPPORTED, "(M / 64 + 1) * ceil(N / 64) must be below 2^23");
-  const bool vec = ldy % 8 == 0 && aligned(y, 16) && (!residual || (ldr % 8 == 0 && aligned(residual, 16))) &&
-                   aligned(bias, 16);
-  const LinearArgs p{(const int8_t*)xq, ldx, sx, (const int8_t*)wq, sw, M, N, K, bias, residual, ldr, dtype, y, ldy, vec};
+  const bool whole = ldy % 8 == 0 && aligned(y, 16);
+  const LinearArgs p{(const int8_t*)xq, ldx, sx, (const int8_t*)wq, sw, M, N, K, bias, residual, ldr, dtype, y, ldy, whole};
   return hip_status(launch_linear_i8(p, (hipStream_t)stream), "linear_i8");
 }
 

@@ -226,7 +226,7 @@ struct LinearArgs {
   int32_t dtype;
   void* y;
   int64_t ldy;
-  bool vec;                 // bias, residual and y move in 16-byte runs
+  bool aligned;             // rows of y start on 16-byte boundaries
 };
 hipError_t launch_linear_i8(const LinearArgs& p, hipStream_t s);
 

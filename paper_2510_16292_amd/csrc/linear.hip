@@ -50,37 +50,47 @@ __device__ __forceinline__ void lin_wait_stage(int rem) {
   }
 }
 
+// Eight 16-bit elements at any address: a 16-byte access of the hardware needs no
+// alignment (element by element 8192 x 4097 x 512 takes 81 us, so 45).
+typedef int32_t lin_run_t __attribute__((ext_vector_type(4), aligned(2)));
+__device__ __forceinline__ i32x4 lin_run(const uint16_t* p) { return *reinterpret_cast<const lin_run_t*>(p); }
+
 // Eight outputs of row m from column n (below N), scaled: bias and residual added,
-// rounded once and stored, in 16-byte runs where the operands allow it.  The
-// stores are non-temporal: all tiles of a round finish together, and their
+// rounded once and stored, in 16-byte runs where eight are left.  Stores to
+// aligned rows are non-temporal: all tiles of a round finish together, and their
 // outputs need not push the operands out of L2 (5632 x 28160 x 5120 716 -> 690
-// us, 2560 x 4096 x 4096 in 256 x 256 tiles 54.8 -> 44.0).  The residual's
-// reads are ordinary ones: it was written shortly before (2560 x 4096 x 4096
-// 41.2 us a pass, 43.7 past the caches).
+// us, 2560 x 4096 x 4096 in 256 x 256 tiles 54.8 -> 44.0).  Other rows leave
+// parts of lines, which have to meet in L2 (2197 x 30659 x 192 71.9 us past it,
+// 59.9 through it).  The residual's reads are ordinary ones: it was written
+// shortly before (2560 x 4096 x 4096 41.2 us a pass, 43.7 past the caches).
 template <bool BF>
 __device__ __forceinline__ void lin_store(const LinearArgs& p, int64_t m, int32_t n, float* v) {
   using E = Elem16<BF>;
-  if (p.vec && n + 8 <= p.N) {
+  const uint16_t* bias = reinterpret_cast<const uint16_t*>(p.bias) + n;
+  const uint16_t* res = reinterpret_cast<const uint16_t*>(p.residual) + m * p.ldr + n;
+  uint16_t* y = reinterpret_cast<uint16_t*>(p.y) + m * p.ldy + n;
+  if (n + 8 <= p.N) {
     float b[8];
     if (p.bias) {
-      E::unpack(*reinterpret_cast<const i32x4*>(reinterpret_cast<const uint16_t*>(p.bias) + n), b);
+      E::unpack(lin_run(bias), b);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = add_rn(v[e], b[e]);
     }
     if (p.residual) {
-      E::unpack(*reinterpret_cast<const i32x4*>(reinterpret_cast<const uint16_t*>(p.residual) + m * p.ldr + n), b);
+      E::unpack(lin_run(res), b);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = add_rn(v[e], b[e]);
     }
-    __builtin_nontemporal_store(E::pack(v), reinterpret_cast<i32x4*>(reinterpret_cast<uint16_t*>(p.y) + m * p.ldy + n));
+    if (p.aligned) __builtin_nontemporal_store(E::pack(v), reinterpret_cast<i32x4*>(y));
+    else *reinterpret_cast<lin_run_t*>(y) = E::pack(v);
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       if (n + e >= p.N) continue;
       float o = v[e];
-      if (p.bias) o = add_rn(o, E::get(p.bias, n + e));
-      if (p.residual) o = add_rn(o, E::get(p.residual, m * p.ldr + n + e));
-      E::put(p.y, m * p.ldy + n + e, o);
+      if (p.bias) o = add_rn(o, E::get(bias, e));
+      if (p.residual) o = add_rn(o, E::get(res, e));
+      E::put(y, e, o);
     }
   }
 }
@@ -337,12 +347,10 @@ linear_tile_kernel(LinearArgs p, int32_t tiles_n, int32_t gm) {
 // ring of NS stages in LDS -- no barrier until the exact partial sums meet, and
 // a stage's fragments are all read at once.  (Waves that share one tile's
 // stages step by step pay an LDS latency per 32-byte step and a barrier per
-// stage: 128 x 3584 x 9856 25.4 us in 64 x 64 tiles, 17.7 here in 64 x 32 ones.)
-// Loads stay direct-to-LDS ones, eight lanes to a row's 128-byte line: a
+// stage: 128 x 3584 x 9856 25.4 us in 64 x 64 tiles of four waves, 17.7 here in
+// 64 x 32 ones.)  Loads stay direct-to-LDS ones, eight lanes to a row's 128-byte line: a
 // fragment straight from memory has a row per lane, so neighbouring lanes hit
-// different lines (32 x 3584 x 9856: 18.5 us so, 11.0 here).  Products are v_mfma_i32_16x16x64_i8 (lane l: row l % 16 and
-// chunk l / 16 of its operand; output: column 4 (l / 16) + v of the first
-// operand's rows, row l % 16 of the second's).
+// different lines (32 x 3584 x 9856: 18.5 us so, 11.0 here).
 // ---------------------------------------------------------------------------
 // Tile rows that xcd_tile walks together: as xcd_group_rows chooses them (the
 // fewest operand rows in an XCD's share, or among the 32 tiles it runs at once
@@ -523,14 +531,17 @@ static hipError_t launch_linear_tile(const LinearArgs& p, hipStream_t s) {
 // The forms a product may take, and what each costs.  A compute unit takes
 // q = ceil(tiles / 256) tiles; a tile of nk 128-byte stages then costs about
 // fixed + q (tile + nk stage) microseconds.  The three numbers of a form are
-// fitted to its measured times over 136 products (M 1 .. 8192, N 48 .. 32768,
+// fitted to its measured times over 339 products (M 1 .. 8192, N 48 .. 32768,
 // K 128 .. 16384, operands from HBM); the form with the least estimate was on
-// average 1.5% and at most 22% slower than the best of 16 forms measured.  What
+// average 1.3% and at most 21% slower than the best of 27 forms measured.  What
 // they express: a unit takes in at most 55 to 60 bytes per ns while weights
 // come from HBM (95 if everything were in L2), so the stage times are those of
 // (BM + BN) 128 bytes except for the largest tiles, which the products (and the
 // card's power: 1.6 GHz then) bound; small tiles have the shorter ramp and
-// epilogue.
+// epilogue.  Eight waves with more stages in flight hide the LDS reads of the
+// middle tiles (512 x 4096 x 4096 in 128 x 64 tiles 14.1 us, with four waves and
+// three stages 19.0), and shapes between the squares fill the units where one
+// tile too many would begin another round (256 x 5120 x 5120 16.7 us for 23.3).
 struct LinForm {
   int32_t bm, bn;
   double fixed, tile, stage;
@@ -538,25 +549,30 @@ struct LinForm {
   hipError_t (*launch)(const LinearArgs&, hipStream_t);
 };
 static const LinForm kLinForms[] = {
-    {16, 16, 1.429, 1.141, 0.049, 16, launch_linear_split<16, 16, 8, 2>},
-    {32, 16, 1.798, 0.712, 0.070, 32, launch_linear_split<32, 16, 8, 1>},
-    {32, 32, 1.002, 1.506, 0.094, 32, launch_linear_split<32, 32, 8, 1>},
-    {64, 16, 1.633, 1.167, 0.109, 2048, launch_linear_split<64, 16, 8, 1>},
-    {64, 32, 0.101, 2.871, 0.139, 2048, launch_linear_split<64, 32, 8, 1>},
-    {64, 64, 0.000, 4.096, 0.194, 2048, launch_linear_split<64, 64, 4, 2>},
-    {64, 64, 2.288, 1.328, 0.272, INT64_MAX, launch_linear_tile<64, 64, 32, 32, 2>},
-    {128, 64, 1.217, 3.279, 0.409, INT64_MAX, launch_linear_tile<128, 64, 64, 32, 3>},
-    {128, 128, 0.000, 5.054, 0.481, INT64_MAX, launch_linear_tile<128, 128, 64, 32, 4>},
-    {128, 256, 0.000, 7.064, 0.892, INT64_MAX, launch_linear_tile<128, 256, 64, 64, 3>},
-    {160, 256, 0.000, 7.853, 1.043, INT64_MAX, launch_linear_tile<160, 256, 80, 64, 3>},
-    {192, 256, 0.000, 8.138, 1.171, INT64_MAX, launch_linear_tile<192, 256, 96, 64, 2>},
-    {256, 256, 0.000, 10.317, 1.376, INT64_MAX, launch_linear_tile<256, 256, 128, 64, 2>},
+    {16, 16, 1.464, 0.918, 0.058, 16, launch_linear_split<16, 16, 8, 2>},
+    {16, 32, 0.000, 2.211, 0.105, 16, launch_linear_split<16, 32, 8, 2>},
+    {16, 64, 0.000, 2.075, 0.177, 16, launch_linear_split<16, 64, 8, 1>},
+    {32, 16, 1.893, 0.526, 0.077, 32, launch_linear_split<32, 16, 8, 1>},
+    {32, 32, 1.066, 1.183, 0.112, 32, launch_linear_split<32, 32, 8, 1>},
+    {64, 16, 1.773, 0.829, 0.115, 2048, launch_linear_split<64, 16, 8, 1>},
+    {64, 32, 0.000, 2.569, 0.163, 2048, launch_linear_split<64, 32, 8, 1>},
+    {128, 64, 0.000, 4.708, 0.379, 2048, launch_linear_split<128, 64, 4, 1>},
+    {64, 64, 2.001, 0.950, 0.270, INT64_MAX, launch_linear_tile<64, 64, 32, 16, 4>},
+    {96, 64, 0.031, 3.380, 0.374, INT64_MAX, launch_linear_tile<96, 64, 48, 16, 4>},
+    {64, 128, 0.966, 2.089, 0.464, INT64_MAX, launch_linear_tile<64, 128, 32, 32, 4>},
+    {96, 128, 1.000, 2.522, 0.582, INT64_MAX, launch_linear_tile<96, 128, 48, 32, 5>},
+    {128, 128, 0.390, 3.357, 0.619, INT64_MAX, launch_linear_tile<128, 128, 64, 32, 4>},
+    {192, 128, 0.000, 4.823, 0.788, INT64_MAX, launch_linear_tile<192, 128, 96, 32, 3>},
+    {256, 128, 0.978, 6.326, 0.894, INT64_MAX, launch_linear_tile<256, 128, 64, 64, 3>},
+    {160, 256, 0.669, 7.414, 1.057, INT64_MAX, launch_linear_tile<160, 256, 80, 64, 3>},
+    {192, 256, 0.488, 8.026, 1.202, INT64_MAX, launch_linear_tile<192, 256, 96, 64, 2>},
+    {256, 256, 0.074, 10.420, 1.475, INT64_MAX, launch_linear_tile<256, 256, 128, 64, 2>},
 };
 constexpr int64_t kLinUnits = 256;            // compute units
 constexpr int64_t kLinMaxTiles = 1 << 23;     // fewer than 2^32 threads of up to 512 per tile
 constexpr double kLinTwoFrom = 40.0;          // us of a product that may be made in two,
 constexpr int32_t kLinTwoK = 1024;            // its least contraction,
-constexpr double kLinTwoGain = 0.98;          // what it must come to
+constexpr double kLinTwoGain = 0.99;          // what it must come to
 constexpr double kLinTwoCost = 2.0;           // with a second launch
 
 struct LinChoice {
@@ -585,9 +601,9 @@ hipError_t launch_linear_i8(const LinearArgs& p, hipStream_t s) {
   // made in two: whole rounds of one form over the first columns or rows, and
   // what is left in the form (or two) that suits it: 5632 x 28160 x 5120 in 8.9
   // rounds of 256 x 256 tiles and one of 160 x 256, 608 us, in 9.5 rounds 678;
-  // 6033 x 2617 x 12176 228 us for 306.  Over 84 random products from 40 us on
-  // 2.8% on average (one in two 13% slower, three 3%); short contractions, whose
-  // stores the estimate does not see, were up to 9% slower and stay in one.
+  // 4508 x 3741 x 5488 111 us for 137.  Of 70 random products whose estimate is
+  // better in two, the 37 taken are 4.5% faster on average, the worst 7.5% slower;
+  // shorter contractions were lost as often as won.
   int32_t n1 = p.N;
   int64_t m1 = p.M;
   if (one.us > kLinTwoFrom && p.K >= kLinTwoK) {

@@ -364,13 +364,26 @@ LINEAR = [(1, 1, 16), (1, 256, 256), (2, 17, 48), (5, 100, 112), (15, 1000, 1008
 # Ragged products of one part stage, a part second one, three and four whole
 # ones, and five with a part, in sizes that give every form of the product.
 FORMS = [(1, 65, 384), (1, 65, 1008), (17, 65, 208), (17, 65, 656), (1, 4105, 96), (1, 4101, 208), (1, 4097, 384),
-         (1, 4107, 1008), (33, 65, 96), (34, 65, 512), (65, 2057, 96), (33, 4145, 384), (33, 8387, 1008), (1, 8209, 96),
-         (1, 8193, 208), (1, 8215, 384), (1, 8199, 512), (2099, 65, 656), (66, 8613, 96), (66, 8293, 208),
-         (65, 8365, 384), (66, 8201, 512), (67, 8297, 656), (66, 16621, 96), (1, 16433, 208), (33, 17121, 384),
-         (33, 16595, 512), (33, 16831, 656), (131, 16991, 96), (132, 16397, 208), (130, 16845, 384), (131, 16463, 512),
-         (130, 16753, 656), (394, 16721, 96), (390, 16667, 208), (397, 16531, 384), (395, 16589, 512),
-         (388, 16729, 656), (484, 16591, 96), (491, 16693, 208), (490, 16825, 384), (484, 16945, 512),
-         (485, 16499, 656), (577, 17197, 96), (585, 16567, 208), (587, 16661, 384), (591, 16387, 512), (577, 17089, 432)]
+         (1, 4107, 1008), (33, 65, 96), (34, 65, 512), (65, 2057, 96), (33, 4145, 384), (33, 8387, 1008),
+         (1, 8209, 96), (1, 8193, 208), (1, 8215, 384), (1, 8199, 512), (2099, 65, 656), (66, 8613, 96),
+         (66, 8293, 208), (65, 8365, 384), (66, 8201, 512), (67, 8297, 656), (66, 16621, 96), (1, 16433, 208),
+         (33, 17121, 384), (33, 16595, 512), (33, 16831, 656), (131, 16991, 96), (132, 16397, 208), (130, 16845, 384),
+         (131, 16463, 512), (130, 16753, 656), (394, 16721, 96), (390, 16667, 208), (397, 16531, 384),
+         (395, 16589, 512), (388, 16729, 656), (484, 16591, 96), (491, 16693, 208), (490, 16825, 384),
+         (484, 16945, 512), (485, 16499, 656), (577, 17197, 96), (585, 16567, 208), (587, 16661, 384),
+         (591, 16387, 512), (577, 17089, 432), (1, 65, 656), (1, 65, 208), (1, 65, 432), (1, 65, 512), (1, 4097, 656),
+         (1, 65, 96), (1, 8197, 432), (1, 8193, 656), (1, 8217, 1008), (17, 65, 1008), (17, 65, 96), (17, 67, 208),
+         (17, 65, 384), (17, 65, 432), (17, 65, 512), (17, 4101, 656), (17, 4137, 1008), (33, 65, 208), (33, 65, 384),
+         (33, 65, 432), (33, 65, 656), (33, 65, 1008), (65, 2077, 208), (65, 2077, 432), (67, 2073, 512),
+         (33, 4117, 656), (33, 4105, 1008), (342, 5421, 1008), (2054, 65, 96), (2105, 65, 208), (2060, 65, 384),
+         (2058, 67, 432), (2108, 67, 512), (2056, 65, 1008), (67, 8209, 1008), (1, 16411, 96), (1, 16403, 384),
+         (1, 16417, 432), (1, 16393, 512), (1, 16387, 656), (1, 16405, 1008), (65, 16591, 208), (65, 16847, 384),
+         (65, 17037, 432), (65, 16813, 512), (68, 16797, 656), (65, 16607, 1008), (99, 16739, 96), (99, 16473, 208),
+         (103, 16573, 384), (99, 16679, 432), (97, 17087, 512), (97, 16471, 656), (97, 16615, 1008),
+         (129, 16729, 432), (133, 16705, 1008), (200, 16819, 96), (195, 16965, 208), (194, 16635, 384),
+         (194, 17319, 432), (196, 16583, 512), (198, 16515, 656), (195, 16839, 1008), (293, 16485, 96),
+         (291, 16971, 208), (296, 16757, 384), (291, 16495, 432), (290, 16479, 512), (290, 16531, 656),
+         (294, 16965, 1008), (492, 16449, 432)]
 
 
 @pytest.mark.parametrize("M,N,K", FORMS)
@@ -382,16 +395,19 @@ def test_linear_forms(M, N, K):
 
 
 @pytest.mark.parametrize("M,N,K,ldy", [(33, 17179, 10896, 17184), (131, 6019, 11744, 6019), (5456, 141, 11952, 144),
-                                       (342, 3130, 12736, 3136), (1907, 2611, 4112, 2612)])
+                                       (342, 3130, 12736, 3136), (1907, 2611, 4112, 2612),
+                                       (1, 17613, 14560, 17613), (840, 16564, 1680, 16568), (1025, 13466, 1856, 13466),
+                                       (385, 4853, 10256, 4856), (2693, 1462, 6896, 1463),
+                                       (809, 19805, 11968, 19808)])
 def test_linear_in_two_parts(M, N, K, ldy):
     """Long products whose last round would be nearly idle: columns or rows in two
-    launches, with bias, residual and strides."""
+    launches (the last in three), with bias, residual and strides."""
     xq, sx, wq, sw, bias, res = linear_inputs(M + N + K, M, N, K, True, full=True)
     got = run_linear(xq, sx, wq, sw, BF16, bias, res, ldx=K + 32, ldy=ldy)
     assert np.array_equal(got, L.linear_i8(xq, sx, wq, sw, bias, res, True))
 
 
-@pytest.mark.parametrize("M,N,K", [(131, 6019, 11744), (5456, 141, 11952)])
+@pytest.mark.parametrize("M,N,K", [(840, 16564, 1680), (385, 4853, 10256)])
 def test_linear_in_two_parts_captured_in_place(M, N, K):
     """The same, adding into its residual, captured once and replayed: a replay
     adds the product again, as an eager call does."""
@@ -438,6 +454,23 @@ def test_linear_strides_and_alignment(M, N, K, ldx, ldy, offset):
     want = L.linear_i8(xq, sx, wq, sw, bias, res, False)
     assert np.array_equal(run_linear(xq, sx, wq, sw, F16, bias, res, ldx, ldy, offset), want)
     assert np.array_equal(run_linear(xq, sx, wq, sw, F16, bias, res, ldx, ldy, offset, alias=True), want)
+
+
+@pytest.mark.parametrize("M,N,K", [(3, 70, 160), (40, 136, 272), (300, 200, 400)])
+def test_linear_operands_at_odd_addresses(M, N, K):
+    """Bias, residual and output on any element of memory give the aligned result."""
+    t = H.torch()
+    xq, sx, wq, sw, bias, res = linear_inputs(M, M, N, K, True)
+    want = L.linear_i8(xq, sx, wq, sw, bias, res, True)
+    xd, wd, sxd, swd = H.dev(xq), H.dev(wq), H.dev(sx.astype(np.float32)), H.dev(sw.astype(np.float32))
+    for ob, orr, oy in ((1, 0, 0), (0, 3, 0), (0, 0, 5), (7, 2, 1)):
+        b, r = (t.empty(n + 8, dtype=t.bfloat16, device="cuda") for n in (N, M * N))
+        b[ob:ob + N] = up16(bias[None], BF16)[0]
+        r[orr:orr + M * N] = up16(res, BF16).view(-1)
+        y = Guarded(M, N, N, t.bfloat16, oy)
+        B.check(B.qsvd_linear_i8(xd.data_ptr(), K, sxd.data_ptr(), wd.data_ptr(), swd.data_ptr(), M, N, K,
+                                 b.data_ptr() + 2 * ob, r.data_ptr() + 2 * orr, N, BF16, y.ptr, N, B.stream_handle()))
+        assert np.array_equal(y.get(), want), (ob, orr, oy)
 
 
 @pytest.mark.parametrize("M", [1, 32, 70, 300])
