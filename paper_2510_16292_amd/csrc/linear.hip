@@ -66,8 +66,8 @@ __device__ __forceinline__ i32x4 lin_run(const uint16_t* p) { return *reinterpre
 template <bool BF>
 __device__ __forceinline__ void lin_store(const LinearArgs& p, int64_t m, int32_t n, float* v) {
   using E = Elem16<BF>;
-  const uint16_t* bias = reinterpret_cast<const uint16_t*>(p.bias) + n;
-  const uint16_t* res = reinterpret_cast<const uint16_t*>(p.residual) + m * p.ldr + n;
+  const uint16_t* bias = p.bias ? reinterpret_cast<const uint16_t*>(p.bias) + n : nullptr;
+  const uint16_t* res = p.residual ? reinterpret_cast<const uint16_t*>(p.residual) + m * p.ldr + n : nullptr;
   uint16_t* y = reinterpret_cast<uint16_t*>(p.y) + m * p.ldy + n;
   if (n + 8 <= p.N) {
     float b[8];
