@@ -391,7 +391,7 @@ qsvd_status qsvd_silu_mul_quantize_act(const void* gate, int64_t ldg, const void
  *             and overlaps no other operand
  * Requires K % 16 == 0, K < 131072, ldx % 16 == 0, ldx <= 2^22, 16-byte aligned
  * xq and wq, (M / 64 + 1) * ceil(N / 64) < 2^23; any N >= 1 and row strides of
- * residual and y (rows of y that start on 16-byte boundaries are stored fastest). */
+ * residual and y (rows of y that start on 128-byte boundaries are stored fastest). */
 qsvd_status qsvd_linear_i8(const void* xq, int64_t ldx, const float* sx, const void* wq, const float* sw,
                            int64_t M, int32_t N, int32_t K, const void* bias, const void* residual,
                            int64_t ldr, int32_t dtype, void* y, int64_t ldy, void* stream);
