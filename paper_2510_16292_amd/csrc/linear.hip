@@ -16,13 +16,12 @@
 #include "common.h"
 #include "elem16.h"
 #include "launch.h"
+#include "linear_plan.h"
 
 namespace qsvd {
 
 typedef __attribute__((address_space(3))) void lin_lds_t;
 typedef __attribute__((address_space(1))) void lin_glb_t;
-
-constexpr int kLinStage = 128;     // contraction bytes per stage: one cache line of every row
 
 // A stage in LDS: rows of 128 bytes, contraction chunk c (16 bytes) of a row in
 // slot c ^ (row / 2 % 8), so that a fragment read (consecutive rows, one
@@ -528,111 +527,24 @@ static hipError_t launch_linear_tile(const LinearArgs& p, hipStream_t s) {
   return hipGetLastError();
 }
 
-// The forms a product may take, and what each costs.  A compute unit takes
-// q = ceil(tiles / 256) tiles; a tile of nk 128-byte stages then costs about
-// fixed + q (tile + nk stage) microseconds.  The three numbers of a form are
-// fitted to its measured times over 339 products (M 1 .. 8192, N 48 .. 32768,
-// K 128 .. 16384, operands from HBM); the form with the least estimate was on
-// average 1.3% and at most 21% slower than the best of 27 forms measured.  What
-// they express: a unit takes in at most 55 to 60 bytes per ns while weights
-// come from HBM (95 if everything were in L2), so the stage times are those of
-// (BM + BN) 128 bytes except for the largest tiles, which the products (and the
-// card's power: 1.6 GHz then) bound; small tiles have the shorter ramp and
-// epilogue.  Eight waves with more stages in flight hide the LDS reads of the
-// middle tiles (512 x 4096 x 4096 in 128 x 64 tiles 14.1 us, with four waves and
-// three stages 19.0), and shapes between the squares fill the units where one
-// tile too many would begin another round (256 x 5120 x 5120 16.7 us for 23.3).
-struct LinForm {
-  int32_t bm, bn;
-  double fixed, tile, stage;
-  int64_t max_m;            // the few-rows forms repeat the weights beyond it
-  hipError_t (*launch)(const LinearArgs&, hipStream_t);
-};
-static const LinForm kLinForms[] = {
-    {16, 16, 1.464, 0.918, 0.058, 16, launch_linear_split<16, 16, 8, 2>},
-    {16, 32, 0.000, 2.211, 0.105, 16, launch_linear_split<16, 32, 8, 2>},
-    {16, 64, 0.000, 2.075, 0.177, 16, launch_linear_split<16, 64, 8, 1>},
-    {32, 16, 1.893, 0.526, 0.077, 32, launch_linear_split<32, 16, 8, 1>},
-    {32, 32, 1.066, 1.183, 0.112, 32, launch_linear_split<32, 32, 8, 1>},
-    {64, 16, 1.773, 0.829, 0.115, 2048, launch_linear_split<64, 16, 8, 1>},
-    {64, 32, 0.000, 2.569, 0.163, 2048, launch_linear_split<64, 32, 8, 1>},
-    {128, 64, 0.000, 4.708, 0.379, 2048, launch_linear_split<128, 64, 4, 1>},
-    {64, 64, 2.001, 0.950, 0.270, INT64_MAX, launch_linear_tile<64, 64, 32, 16, 4>},
-    {96, 64, 0.031, 3.380, 0.374, INT64_MAX, launch_linear_tile<96, 64, 48, 16, 4>},
-    {64, 128, 0.966, 2.089, 0.464, INT64_MAX, launch_linear_tile<64, 128, 32, 32, 4>},
-    {96, 128, 1.000, 2.522, 0.582, INT64_MAX, launch_linear_tile<96, 128, 48, 32, 5>},
-    {128, 128, 0.390, 3.357, 0.619, INT64_MAX, launch_linear_tile<128, 128, 64, 32, 4>},
-    {192, 128, 0.000, 4.823, 0.788, INT64_MAX, launch_linear_tile<192, 128, 96, 32, 3>},
-    {256, 128, 0.978, 6.326, 0.894, INT64_MAX, launch_linear_tile<256, 128, 64, 64, 3>},
-    {160, 256, 0.669, 7.414, 1.057, INT64_MAX, launch_linear_tile<160, 256, 80, 64, 3>},
-    {192, 256, 0.488, 8.026, 1.202, INT64_MAX, launch_linear_tile<192, 256, 96, 64, 2>},
-    {256, 256, 0.074, 10.420, 1.475, INT64_MAX, launch_linear_tile<256, 256, 128, 64, 2>},
-};
-constexpr int64_t kLinUnits = 256;            // compute units
-constexpr int64_t kLinMaxTiles = 1 << 23;     // fewer than 2^32 threads of up to 512 per tile
-constexpr double kLinTwoFrom = 40.0;          // us of a product that may be made in two,
-constexpr int32_t kLinTwoK = 1024;            // its least contraction,
-constexpr double kLinTwoGain = 0.99;          // what it must come to
-constexpr double kLinTwoCost = 2.0;           // with a second launch
-
-struct LinChoice {
-  const LinForm* form;      // NULL: none
-  double us;
-};
-static int64_t lin_tiles(int64_t n, int32_t b) { return (n + b - 1) / b; }
-
-static LinChoice lin_choose(int64_t M, int32_t N, int32_t K) {
-  LinChoice best{nullptr, 0.0};
-  const double nk = (double)lin_tiles(K, kLinStage);
-  for (const LinForm& f : kLinForms) {
-    const int64_t tiles = lin_tiles(M, f.bm) * lin_tiles(N, f.bn);
-    if (M > f.max_m || tiles >= kLinMaxTiles) continue;
-    const double us = f.fixed + (double)lin_tiles(tiles, kLinUnits) * (f.tile + nk * f.stage);
-    if (!best.form || us < best.us) best = LinChoice{&f, us};
-  }
-  return best;
-}
+// The launcher of each form, in the order of kLinForms.
+#define QSVD_LIN_SPLIT(bm, bn, nw, ns, ...) launch_linear_split<bm, bn, nw, ns>,
+#define QSVD_LIN_TILE(bm, bn, wm, wn, ns, ...) launch_linear_tile<bm, bn, wm, wn, ns>,
+static hipError_t (*const kLinLaunch[])(const LinearArgs&, hipStream_t) = {
+    QSVD_LINEAR_FORMS(QSVD_LIN_SPLIT, QSVD_LIN_TILE)};
+#undef QSVD_LIN_SPLIT
+#undef QSVD_LIN_TILE
 
 hipError_t launch_linear_i8(const LinearArgs& p, hipStream_t s) {
   if (p.M == 0) return hipSuccess;
-  LinChoice one = lin_choose(p.M, p.N, p.K);
-  if (!one.form) return hipErrorInvalidConfiguration;
-  // A long product whose tiles leave most units idle in their last round is
-  // made in two: whole rounds of one form over the first columns or rows, and
-  // what is left in the form (or two) that suits it: 5632 x 28160 x 5120 in 8.9
-  // rounds of 256 x 256 tiles and one of 160 x 256, 608 us, in 9.5 rounds 678;
-  // 4508 x 3741 x 5488 111 us for 137.  Of 70 random products whose estimate is
-  // better in two, the 37 taken are 4.5% faster on average, the worst 7.5% slower;
-  // shorter contractions were lost as often as won.
-  int32_t n1 = p.N;
-  int64_t m1 = p.M;
-  if (one.us > kLinTwoFrom && p.K >= kLinTwoK) {
-    double least = kLinTwoGain * one.us - kLinTwoCost;
-    const double nk = (double)lin_tiles(p.K, kLinStage);
-    const LinForm* first = nullptr;
-    for (const LinForm& f : kLinForms) {
-      const int64_t tm = lin_tiles(p.M, f.bm), tn = lin_tiles(p.N, f.bn), rounds = lin_tiles(tm * tn, kLinUnits) - 1;
-      if (p.M > f.max_m || tm * tn >= kLinMaxTiles || rounds < 1) continue;
-      const double us = f.fixed + (double)rounds * (f.tile + nk * f.stage);
-      const int64_t cols = rounds * kLinUnits / tm * f.bn, rws = rounds * kLinUnits / tn * f.bm;
-      for (int by_rows = 0; by_rows < 2; ++by_rows) {
-        if (by_rows ? rws < 1 || rws >= p.M : cols < 1 || cols >= p.N) continue;
-        const LinChoice rest = by_rows ? lin_choose(p.M - rws, p.N, p.K) : lin_choose(p.M, (int32_t)(p.N - cols), p.K);
-        if (!rest.form || us + rest.us >= least) continue;
-        least = us + rest.us;
-        first = &f;
-        m1 = by_rows ? rws : p.M;
-        n1 = by_rows ? p.N : (int32_t)cols;
-      }
-    }
-    if (first) one.form = first;
-  }
+  const LinPart first = lin_first_part(p.M, p.N, p.K);
+  if (first.form < 0) return hipErrorInvalidConfiguration;
   LinearArgs a = p;
-  a.M = m1;
-  a.N = n1;
-  if (hipError_t e = one.form->launch(a, s); e != hipSuccess || (m1 == p.M && n1 == p.N)) return e;
-  const int64_t m0 = m1 < p.M ? m1 : 0;
-  const int32_t n0 = n1 < p.N ? n1 : 0;
+  a.M = first.m;
+  a.N = first.n;
+  if (hipError_t e = kLinLaunch[first.form](a, s); e != hipSuccess || (a.M == p.M && a.N == p.N)) return e;
+  const int64_t m0 = first.m < p.M ? first.m : 0;
+  const int32_t n0 = first.n < p.N ? first.n : 0;
   a.M = p.M - m0;
   a.N = p.N - n0;
   a.x = p.x + m0 * p.ldx;
