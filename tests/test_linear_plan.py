@@ -100,3 +100,21 @@ def test_every_launch_is_within_its_form(plan):
             assert -(-pm // bm) * -(-pn // bn) < 1 << 23
             area += pm * pn
         assert area == m * n
+
+
+def cuts(size, parts):
+    m, n, _ = size
+    out = ""
+    for _, pm, pn in parts[:-1]:
+        assert (pm < m) != (pn < n)
+        out += "r" if pm < m else "c"
+        m, n = (m - pm, n) if pm < m else (m, n - pn)
+    assert parts[-1][1:] == (m, n)
+    return out
+
+
+def test_part_shapes_are_cut_as_stated(plan):
+    _, parts = plan([s[:3] for s in S.PARTS])
+    for s, p in zip(S.PARTS, parts):
+        assert cuts(s[:3], p) == s[3], s
+    assert {s[3] for s in S.PARTS} >= {"r", "c", "rc", "cr", "cc"}
