@@ -350,8 +350,9 @@ size_t qsvd_decode_workspace_size(const qsvd_layer* w, const qsvd_cache* c, int3
  *   xq        device int8 [M][K] or packed int4 [M][K/2], and sx device fp32
  *             [M], or both NULL; y or xq must be given
  * Apart from h as stated, outputs do not overlap inputs or each other.
- * A row whose a = clip * max |y| is below 2^-119 (Qm / a passes fp32) has scale
- * 1 and codes 0, as an all-zero row has; a row with a y that is not finite (an
+ * A row whose a = clip * max |y| is below 2^-119 has scale 1 and codes 0, as an
+ * all-zero row has (scales a / 127 then stay normal fp32 numbers, 2^-126 and
+ * above; the bound is the same for 4 bits); a row with a y that is not finite (an
  * infinity or NaN in x, a sum past dtype) has scale NaN and codes 0, and other
  * rows are not affected.
  * Requires K % 8 == 0, K <= 65536, M < 2^22, strides that are multiples of 8,

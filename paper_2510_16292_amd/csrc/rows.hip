@@ -21,8 +21,10 @@ constexpr int kRowMaxWaves = 16;
 constexpr int kPackThreads = 256;
 
 // The scale of a row with a = clip * max |y|, and what its values are
-// multiplied by: a row whose Qm / a would pass fp32 counts as all zero; one
-// that holds a value that is not finite gets scale NaN.  Both have codes 0.
+// multiplied by: a row with a below 2^-119 counts as all zero, so that scales
+// a / 127 are normal numbers (2^-126 and above; Qm / a is far from passing
+// fp32); one that holds a value that is not finite gets scale NaN.  Both have
+// codes 0.
 struct RowScale {
   float inv, s;
 };
