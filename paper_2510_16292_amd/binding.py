@@ -217,9 +217,10 @@ def stream_handle(stream=None):
     import torch
     if stream is not None:
         return stream.cuda_stream
-    if not torch.cuda.is_initialized():
-        torch.cuda.init()
-    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    if raw is None:                                     # not a public function of torch
+        return torch.cuda.current_stream().cuda_stream
+    return raw(torch.cuda.current_device())
 
 
 class DeviceLayer:
