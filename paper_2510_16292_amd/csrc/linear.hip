@@ -214,7 +214,7 @@ linear_tile_kernel(LinearArgs p, int32_t tiles_n, int32_t gm) {
       product(kk, t);
 #pragma unroll
       for (int q = 0; q < NR; ++q)
-        if (q * NP / NR / 2 == t || (NR > NP && t == NP - 1 && q * NP / NR / 2 > t)) read_one(st_read, 1 - kk, q);
+        if (q * NP / NR / 2 == t) read_one(st_read, 1 - kk, q);
       if (loads)
 #pragma unroll
         for (int j = 0; j < C::kLPW; ++j)
