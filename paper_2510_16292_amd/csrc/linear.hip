@@ -55,13 +55,16 @@ typedef int32_t lin_run_t __attribute__((ext_vector_type(4), aligned(2)));
 __device__ __forceinline__ i32x4 lin_run(const uint16_t* p) { return *reinterpret_cast<const lin_run_t*>(p); }
 
 // Eight outputs of row m from column n (below N), scaled: bias and residual added,
-// rounded once and stored, in 16-byte runs where eight are left.  Stores to
-// aligned rows are non-temporal: all tiles of a round finish together, and their
-// outputs need not push the operands out of L2 (5632 x 28160 x 5120 716 -> 690
-// us, 2560 x 4096 x 4096 in 256 x 256 tiles 54.8 -> 44.0).  Other rows leave
-// parts of lines, which have to meet in L2 (2197 x 30659 x 192 71.9 us past it,
-// 59.9 through it).  The residual's reads are ordinary ones: it was written
-// shortly before (2560 x 4096 x 4096 41.2 us a pass, 43.7 past the caches).
+// rounded once and stored, in 16-byte runs where eight are left.  Stores to rows
+// that start on 16-byte boundaries are non-temporal: all tiles of a round finish
+// together, and their outputs need not push the operands out of L2 (5632 x 28160 x
+// 5120 716 -> 690 us, 2560 x 4096 x 4096 in 256 x 256 tiles 54.8 -> 44.0).  Other
+// rows leave parts of 16-byte runs, which have to meet in L2 (2197 x 30659 x 192 71.9
+// us past it, 59.9 through it).  Rows in between, of whole runs but parts of 128-byte
+// lines, go either way, past L2 / through it: 5632 x 5128 x 5120 136 / 146 us, 8192 x
+// 4128 x 512 36.0 / 41.8, 100000 x 520 x 128 46.9 / 53.3, but 4000 x 8200 x 256 34.9 /
+// 33.4 and 2197 x 30664 x 192 65.8 / 54.3.  The residual's reads are ordinary ones: it
+// was written shortly before (2560 x 4096 x 4096 41.2 us a pass, 43.7 past the caches).
 template <bool BF>
 __device__ __forceinline__ void lin_store(const LinearArgs& p, int64_t m, int32_t n, float* v) {
   using E = Elem16<BF>;
@@ -340,6 +343,15 @@ linear_tile_kernel(LinearArgs p, int32_t tiles_n, int32_t gm) {
   }
 }
 
+// Tile rows that xcd_tile walks together: as xcd_group_rows chooses them (the
+// fewest operand rows in an XCD's share, or among the 32 tiles it runs at once
+// where the share is many times that), without its search over the tile rows.
+static int lin_group_rows(int64_t tiles_m, int64_t tiles_n) {
+  const double share = (double)(tiles_m * tiles_n) / 8;
+  const double g = share > 128 && tiles_n >= 6 ? 5.0 : sqrt(share);
+  return (int)(g < 1.0 ? 1.0 : g > (double)tiles_m ? (double)tiles_m : g + 0.5);
+}
+
 // ---------------------------------------------------------------------------
 // Few tiles: BM x BN outputs per workgroup, its NW waves taking the stages in
 // turn (wave w stages w, w + NW, ...), each over the whole tile with a private
@@ -351,15 +363,6 @@ linear_tile_kernel(LinearArgs p, int32_t tiles_n, int32_t gm) {
 // fragment straight from memory has a row per lane, so neighbouring lanes hit
 // different lines (32 x 3584 x 9856: 18.5 us so, 11.0 here).
 // ---------------------------------------------------------------------------
-// Tile rows that xcd_tile walks together: as xcd_group_rows chooses them (the
-// fewest operand rows in an XCD's share, or among the 32 tiles it runs at once
-// where the share is many times that), without its search over the tile rows.
-static int lin_group_rows(int64_t tiles_m, int64_t tiles_n) {
-  const double share = (double)(tiles_m * tiles_n) / 8;
-  const double g = share > 128 && tiles_n >= 6 ? 5.0 : sqrt(share);
-  return (int)(g < 1.0 ? 1.0 : g > (double)tiles_m ? (double)tiles_m : g + 0.5);
-}
-
 template <int N>
 __device__ __forceinline__ void lin_wait_loads() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");

@@ -17,9 +17,9 @@ constexpr int kLinStage = 128;     // contraction bytes per stage: one cache lin
 // come from HBM (95 if everything were in L2), so the stage times are those of
 // (BM + BN) 128 bytes except for the largest tiles, which the products (and the
 // card's power: 1.6 GHz then) bound; small tiles have the shorter ramp and
-// epilogue.  Eight waves with more stages in flight hide the LDS reads of the
-// middle tiles (512 x 4096 x 4096 in 128 x 64 tiles 14.1 us, with four waves and
-// three stages 19.0), and shapes between the squares fill the units where one
+// epilogue.  Eight waves hide the LDS reads of the middle tiles (in 64 x 64 ones
+// 160 x 4096 x 4096 9.7 us, with four waves and as many stages 12.3; 710 x 714 x
+// 14848 23.8 for 33.5), and shapes between the squares fill the units where one
 // tile too many would begin another round (256 x 5120 x 5120 16.7 us for 23.3).
 //
 //   S(BM, BN, NW, NS, ...)       linear_split_kernel
@@ -96,8 +96,9 @@ struct LinPart {
 // A long product whose tiles leave most units idle in their last round is
 // made in two: whole rounds of one form over the first columns or rows, and
 // what is left in the form (or two) that suits it: 5632 x 28160 x 5120 in 8.9
-// rounds of 256 x 256 tiles and one of 160 x 256, 608 us, in 9.5 rounds 678;
-// 4508 x 3741 x 5488 111 us for 137.  Of 70 random products whose estimate is
+// rounds of 256 x 256 tiles and one of 160 x 256 683 us, in 9.5 rounds 709 (codes
+// of the full range; 643 on quantized normal ones); 640 x 22528 x 4096 66.8 us for
+// 79.4; 4508 x 3741 x 5488 110 for 131.  Of 70 random products whose estimate is
 // better in two, the 37 taken are 4.5% faster on average, the worst 7.5% slower;
 // shorter contractions were lost as often as won.
 inline LinPart lin_first_part(int64_t M, int32_t N, int32_t K) {
