@@ -255,12 +255,15 @@ silu_mul_quantize_kernel(GateArgs a, int lane_bits) {
 // with eight waves for five, 50.6 at one chunk.  Rows of one wave take one chunk
 // (8192 x 256 norms 6.5 us, 7.8 at two); for two to four waves of one chunk it is
 // the same within 5% (65536 x 1024 norms 106 us for 115, 8192 x 1024 gates 13.2 for
-// 12.4); rows past 16 waves of two take four or eight (512 x 32768 gates 19.8 us,
-// 100 x 65536 norms 25.3).  Rows of half a wave or less share waves: a workgroup
-// costs 0.4 ns whatever is in it (65536 norms of 64 elements 9.8 us for 30.0, of
-// 128 16.5 for 31.3, of 256 31.6 for 33.0, gates of 64 8.5 for 25.9, 4 us of each
-// the timing's own).  Whole waves gain nothing from sharing a workgroup (262144 norms of
-// 512 187 us for 180, gates 141 for 149).
+// 12.4); rows past 16 waves of two take four (512 x 32768 gates 19.8 us, 2000 x
+// 32768 norms 96.9, 4.7 TB/s) or eight.  Eight do not fit the registers of a norm
+// (the compiler spills 23 of them in fp16 and 183 in bf16): 2000 x 65536 norms reach
+// 3.7 and 2.2 TB/s, gates, which spill none, 4.9.  Rows of half a wave or less
+// share waves: a workgroup costs 0.4 ns whatever is in it (65536 norms of 64
+// elements 9.8 us for 30.0, of 128 16.5 for 31.3, of 256 31.6 for 33.0, gates of
+// 64 8.5 for 25.9, 4 us of each the timing's own).  Whole waves gain nothing
+// from sharing a workgroup (262144 norms of 512 187 us for 180, gates 141 for
+// 149).
 struct RowShape {
   unsigned grid, threads;
   int lane_bits;            // of packed rows
