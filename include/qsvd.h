@@ -397,6 +397,129 @@ qsvd_status qsvd_linear_i8(const void* xq, int64_t ldx, const float* sx, const v
                            int64_t M, int32_t N, int32_t K, const void* bias, const void* residual,
                            int64_t ldr, int32_t dtype, void* y, int64_t ldy, void* stream);
 
+/* ---- Rotary layers: positions on several axes and a paged key/value cache ----
+ * A rotary key depends on its position, so a latent cache makes every step
+ * rebuild all keys; with few key/value heads a token's K and V are also no
+ * wider than its latent (2 * 4 heads of 128: r = 1024).  For such layers these
+ * calls turn Q and K once, keep K and V of every token in pages (16-bit rows,
+ * or int8 / int4 codes with a scale per token and head), and attend over the
+ * pages.  A layer's step: qsvd_lowrank_qkv_prefill (Q, K, V), qsvd_rope_axes,
+ * qsvd_paged_append, qsvd_paged_attention, qsvd_linear_i8.  `dtype`
+ * (QSVD_F16 or QSVD_BF16) is the type of every 16-bit operand. */
+
+enum { QSVD_ROPE_MAX_AXES = 4 };
+
+/* How the frequencies of a rotary embedding go with the axes of a position.
+ * The head_dim / 2 pairs (j, j + head_dim / 2) are dealt to the axes in runs:
+ * section[0] pairs to axis 0, the next section[1] to axis 1, and so on.
+ *   QSVD_ROPE_RUNNING  pair j turns by pos * theta^(-2j / head_dim), whatever its axis
+ *   QSVD_ROPE_RESTART  the i-th pair of an axis with n pairs turns by pos * theta^(-i / n):
+ *                      every axis has the whole range of frequencies */
+enum { QSVD_ROPE_RUNNING = 0, QSVD_ROPE_RESTART = 1 };
+typedef struct {
+  int32_t head_dim;
+  int32_t n_axes;                        /* 1 .. QSVD_ROPE_MAX_AXES */
+  int32_t section[QSVD_ROPE_MAX_AXES];   /* pairs of each axis, summing to head_dim / 2 */
+  int32_t order;                         /* QSVD_ROPE_RUNNING or QSVD_ROPE_RESTART */
+  float   theta;                         /* finite, > 1 */
+} qsvd_rope;
+
+/* Rotary embedding of M rows of query heads and, optionally, of key heads at
+ * positions with several axes: with x, y the elements j and j + head_dim / 2 of
+ * a head vector and a its angle, x cos a - y sin a and y cos a + x sin a, each
+ * rounded to dtype once.  The angle is formed in revolutions and reduced to
+ * [0, 1) in fp64, its sine and cosine taken in fp32 (the hardware's, about
+ * 2^-20 absolute).  With the same position on every axis, QSVD_ROPE_RUNNING is
+ * the one-axis embedding.  Any int32 position (negative ones turn back).
+ *   pos     device int32 [n_axes][ldpos]: row m of axis a at pos[a * ldpos + m]
+ *   q       device [M][ldq], the n_q_heads heads of a row next to each other
+ *   q_out   device [M][ldqo]; may be q itself (same address and stride)
+ *   k, k_out  the same for the keys, or both NULL (n_k_heads 0)
+ * Requires head_dim a multiple of 16 up to 256, n_q_heads + n_k_heads <= 256,
+ * M < 2^22, 16-byte aligned rows (strides that are multiples of 8). */
+qsvd_status qsvd_rope_axes(const qsvd_rope* rope, const int32_t* pos, int64_t ldpos, int64_t M, int32_t dtype,
+                           const void* q, int64_t ldq, int32_t n_q_heads, void* q_out, int64_t ldqo,
+                           const void* k, int64_t ldk, int32_t n_k_heads, void* k_out, int64_t ldko,
+                           void* stream);
+
+/* The pages of one layer's keys and values.  A page holds page_size
+ * consecutive tokens of one sequence, every head's rows together:
+ *   F16   k, v are [n_pages][n_kv_heads][page_size][head_dim] of dtype, scales NULL
+ *   I8    ... int8 codes, I4 packed int4 codes ([head_dim / 2] bytes), and
+ *         k_scale, v_scale are fp32 [n_pages][n_kv_heads][page_size] */
+typedef struct {
+  int32_t fmt;         /* QSVD_CACHE_*; F16 means rows of dtype */
+  int32_t dtype;       /* type of K, V, Q and the outputs, and of F16 rows */
+  int32_t n_kv_heads;
+  int32_t head_dim;    /* 64 or 128 */
+  int32_t page_size;   /* tokens: a power of two, 16 to 1024 */
+  int32_t n_pages;
+  void*   k;           /* device */
+  void*   v;           /* device */
+  float*  k_scale;     /* device or NULL (F16) */
+  float*  v_scale;
+} qsvd_pages;
+
+/* What one step brings to `batch` sequences; every layer of the step uses the
+ * same.  Token t of sequence b is in page page_table[b][t / page_size], row
+ * t % page_size.  The step's new tokens are the last ones of each sequence:
+ * rows first[b] .. first[b + 1] - 1 of Q, K, V and the outputs, at positions
+ * seq_len[b] - (first[b + 1] - first[b]) .. seq_len[b] - 1.
+ * A row whose position is negative, or whose page_table column is past
+ * max_pages or names no page in [0, n_pages), has no place: it is not written,
+ * reads as zeros, and as a key or value is not there (masked).  Rows at or
+ * past first[batch] or n_rows are left alone. */
+typedef struct {
+  int32_t batch;
+  int32_t max_pages;           /* columns of page_table */
+  const int32_t* page_table;   /* device [batch][max_pages] */
+  const int32_t* seq_len;      /* device [batch]: tokens after the step */
+  const int32_t* first;        /* device [batch + 1], nondecreasing, first[0] = 0 */
+  int32_t max_len;             /* host: at least every seq_len[b] (sizes launches) */
+  int32_t max_new;             /* host: at least every first[b + 1] - first[b] */
+  int64_t n_rows;              /* host: rows of Q, K, V and the outputs */
+} qsvd_page_batch;
+
+/* Write the step's new key and value rows into their pages.  I8 / I4: per row
+ * and head, a = fp32(clip * max |x|) and scale = a / Qm, the code of x the
+ * integer nearest to x * Qm / a within [-Qm, Qm], ties to even (the quotient is
+ * formed so that one half way between two integers is met exactly); a below
+ * 2^-119 gives scale 1 and codes 0, a value that is not finite gives its row and
+ * head scale NaN and codes 0.  F16 rows are copied.
+ *   k, v  device [n_rows][ldk], [n_rows][ldv], heads next to each other
+ * Lengths and tables are not changed: the caller advances seq_len before the
+ * step, once for all layers.  If two rows have the same place, either may stay.
+ * Requires n_kv_heads <= 256, n_rows < 2^22, batch <= 65536, 16-byte aligned
+ * rows and pages, 0 < clip <= 1. */
+qsvd_status qsvd_paged_append(const qsvd_pages* pages, const qsvd_page_batch* batch, const void* k, int64_t ldk,
+                              const void* v, int64_t ldv, float clip, void* stream);
+
+/* Read the rows at the step's positions back out of their pages, as dtype:
+ * code * scale in fp32, rounded once.  (A batch whose new tokens are all of a
+ * sequence's reads the whole sequence.)  Arguments as for qsvd_paged_append. */
+qsvd_status qsvd_paged_read(const qsvd_pages* pages, const qsvd_page_batch* batch, void* k, int64_t ldk, void* v,
+                            int64_t ldv, void* stream);
+
+/* Causal attention of the step's new tokens over their sequences' pages
+ * (append first, then attend): the query at position p sees the keys at
+ * positions 0 .. p that are there; softmax(q k^T * sm_scale) v with fp32
+ * statistics, query head h reading key/value head h / (n_q_heads /
+ * n_kv_heads).  A query that sees no key gets zeros.  One token per sequence
+ * (decode), chunks of a prompt, whole prompts, or all of them in one batch.
+ *   q, out    device [n_rows][ldq], [n_rows][ldo], n_q_heads heads of head_dim
+ *   sm_scale  0 selects 1/sqrt(head_dim)
+ *   ws        device workspace of at least the size query's bytes
+ * A key or value row that is NaN or infinite reaches only queries that see it.
+ * Calls that may overlap need workspaces of their own.  Lengths are read on the
+ * device: a captured call may be replayed with other lengths up to max_len and
+ * max_new.  A call repeats exactly for the same arguments.
+ * Requires n_q_heads a multiple of n_kv_heads and at most 256, batch <= 65536,
+ * n_rows < 2^22, 16-byte aligned rows, pages and ws. */
+qsvd_status qsvd_paged_attention(const qsvd_pages* pages, const qsvd_page_batch* batch, const void* q, int64_t ldq,
+                                 int32_t n_q_heads, float sm_scale, void* out, int64_t ldo, void* ws, size_t ws_bytes,
+                                 void* stream);
+size_t qsvd_paged_attention_workspace_size(const qsvd_pages* pages, const qsvd_page_batch* batch, int32_t n_q_heads);
+
 const char* qsvd_status_string(qsvd_status s);
 const char* qsvd_last_error(void);
 

@@ -17,6 +17,8 @@ QSVD_CACHE_F16, QSVD_CACHE_I8, QSVD_CACHE_I4 = 0, 1, 2
 QSVD_ATTN_AUTO, QSVD_ATTN_ABSORBED, QSVD_ATTN_RECONSTRUCT = 0, 1, 2
 QSVD_OUT_Q, QSVD_OUT_K, QSVD_OUT_V = 1, 2, 4
 QSVD_F16, QSVD_BF16 = 0, 1
+QSVD_ROPE_RUNNING, QSVD_ROPE_RESTART = 0, 1
+QSVD_ROPE_MAX_AXES = 4
 
 EXPORTED = [
     "qsvd_quantize_act", "qsvd_quantize_act_rotated", "qsvd_lowrank_qkv_prefill", "qsvd_prefill_workspace_size",
@@ -26,6 +28,8 @@ EXPORTED = [
     "qsvd_latent_decode_attention_rope",
     "qsvd_decode_workspace_size", "qsvd_latent_decode_attention_noalloc", "qsvd_noalloc_scratch_bytes",
     "qsvd_rmsnorm_quantize_act", "qsvd_silu_mul_quantize_act", "qsvd_linear_i8",
+    "qsvd_rope_axes", "qsvd_paged_append", "qsvd_paged_read", "qsvd_paged_attention",
+    "qsvd_paged_attention_workspace_size",
     "qsvd_status_string", "qsvd_last_error", "qsvd_profile_enable", "qsvd_profile_reset",
     "qsvd_profile_read",
 ]
@@ -48,6 +52,29 @@ class QsvdCache(ctypes.Structure):
     ]
 
 
+class QsvdRope(ctypes.Structure):
+    _fields_ = [
+        ("head_dim", ctypes.c_int32), ("n_axes", ctypes.c_int32), ("section", ctypes.c_int32 * QSVD_ROPE_MAX_AXES),
+        ("order", ctypes.c_int32), ("theta", ctypes.c_float),
+    ]
+
+
+class QsvdPages(ctypes.Structure):
+    _fields_ = [
+        ("fmt", ctypes.c_int32), ("dtype", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+    ]
+
+
+class QsvdPageBatch(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("page_table", ctypes.c_void_p),
+        ("seq_len", ctypes.c_void_p), ("first", ctypes.c_void_p), ("max_len", ctypes.c_int32),
+        ("max_new", ctypes.c_int32), ("n_rows", ctypes.c_int64),
+    ]
+
+
 class QsvdError(RuntimeError):
     def __init__(self, status, message):
         super().__init__(f"{status_string(status)} ({status}): {message}")
@@ -67,6 +94,7 @@ def lib():
         P, I32, I64, U32, SZ, F = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_uint32,
                                     ctypes.c_size_t, ctypes.c_float)
         LP, CP = ctypes.POINTER(QsvdLayer), ctypes.POINTER(QsvdCache)
+        RP, GP, BP = ctypes.POINTER(QsvdRope), ctypes.POINTER(QsvdPages), ctypes.POINTER(QsvdPageBatch)
         sig = {
             "qsvd_quantize_act": (I32, [P, I64, I32, I64, I32, F, P, P, P]),
             "qsvd_quantize_act_rotated": (I32, [P, I64, I32, I64, I32, F, P, I32, P, P, P]),
@@ -84,6 +112,11 @@ def lib():
             "qsvd_rmsnorm_quantize_act": (I32, [P, I64, P, I64, P, I64, I32, I32, F, I32, F, P, I64, P, I64, P, P, P]),
             "qsvd_silu_mul_quantize_act": (I32, [P, I64, P, I64, I64, I32, I32, I32, F, P, P, P]),
             "qsvd_linear_i8": (I32, [P, I64, P, P, P, I64, I32, I32, P, P, I64, I32, P, I64, P]),
+            "qsvd_rope_axes": (I32, [RP, P, I64, I64, I32, P, I64, I32, P, I64, P, I64, I32, P, I64, P]),
+            "qsvd_paged_append": (I32, [GP, BP, P, I64, P, I64, F, P]),
+            "qsvd_paged_read": (I32, [GP, BP, P, I64, P, I64, P]),
+            "qsvd_paged_attention": (I32, [GP, BP, P, I64, I32, F, P, I64, P, SZ, P]),
+            "qsvd_paged_attention_workspace_size": (SZ, [GP, BP, I32]),
             "qsvd_status_string": (ctypes.c_char_p, [I32]),
             "qsvd_last_error": (ctypes.c_char_p, []),
             "qsvd_profile_enable": (I32, [I32, ctypes.c_char_p]),
@@ -174,6 +207,28 @@ def qsvd_silu_mul_quantize_act(gate, ldg, up, ldu, M, K, dtype, bits, clip, xq, 
 
 def qsvd_linear_i8(xq, ldx, sx, wq, sw, M, N, K, bias, residual, ldr, dtype, y, ldy, stream):
     return lib().qsvd_linear_i8(xq, ldx, sx, wq, sw, M, N, K, bias, residual, ldr, dtype, y, ldy, stream)
+
+
+def qsvd_rope_axes(rope, pos, ldpos, M, dtype, q, ldq, n_q_heads, q_out, ldqo, k, ldk, n_k_heads, k_out, ldko, stream):
+    return lib().qsvd_rope_axes(ctypes.byref(rope), pos, ldpos, M, dtype, q, ldq, n_q_heads, q_out, ldqo, k, ldk,
+                                n_k_heads, k_out, ldko, stream)
+
+
+def qsvd_paged_append(pages, batch, k, ldk, v, ldv, clip, stream):
+    return lib().qsvd_paged_append(ctypes.byref(pages), ctypes.byref(batch), k, ldk, v, ldv, clip, stream)
+
+
+def qsvd_paged_read(pages, batch, k, ldk, v, ldv, stream):
+    return lib().qsvd_paged_read(ctypes.byref(pages), ctypes.byref(batch), k, ldk, v, ldv, stream)
+
+
+def qsvd_paged_attention(pages, batch, q, ldq, n_q_heads, sm_scale, out, ldo, ws, ws_bytes, stream):
+    return lib().qsvd_paged_attention(ctypes.byref(pages), ctypes.byref(batch), q, ldq, n_q_heads, sm_scale, out, ldo,
+                                      ws, ws_bytes, stream)
+
+
+def qsvd_paged_attention_workspace_size(pages, batch, n_q_heads):
+    return lib().qsvd_paged_attention_workspace_size(ctypes.byref(pages), ctypes.byref(batch), n_q_heads)
 
 
 def status_string(status):
@@ -296,6 +351,54 @@ class DeviceCache:
             self.scale.copy_(snap["scale"])
         self.seq_len.copy_(snap["seq_len"])
         self.c.max_len = snap["max_len"]
+
+
+def rope(head_dim, section, theta, order=QSVD_ROPE_RUNNING):
+    """The qsvd_rope struct of an embedding whose pairs go to the axes in runs of
+    ``section`` pairs."""
+    section = list(section)
+    if not 1 <= len(section) <= QSVD_ROPE_MAX_AXES:
+        raise ValueError(f"1 to {QSVD_ROPE_MAX_AXES} axes, not {len(section)}")
+    return QsvdRope(head_dim, len(section), (ctypes.c_int32 * QSVD_ROPE_MAX_AXES)(*section), order, theta)
+
+
+class DevicePages:
+    """One layer's paged key/value cache in device memory; ``.c`` is the
+    qsvd_pages struct."""
+
+    def __init__(self, fmt, dtype, n_pages, page_size, n_kv_heads, head_dim, device="cuda"):
+        import torch
+        self.fmt, self.dtype, self.n_pages, self.page_size = fmt, dtype, n_pages, page_size
+        self.n_kv_heads, self.head_dim = n_kv_heads, head_dim
+        element = {QSVD_CACHE_F16: torch.bfloat16 if dtype == QSVD_BF16 else torch.float16,
+                   QSVD_CACHE_I8: torch.int8, QSVD_CACHE_I4: torch.uint8}[fmt]
+        shape = (n_pages, n_kv_heads, page_size, head_dim // 2 if fmt == QSVD_CACHE_I4 else head_dim)
+        self.k = torch.zeros(shape, dtype=element, device=device)
+        self.v = torch.zeros(shape, dtype=element, device=device)
+        self.k_scale = self.v_scale = None
+        if fmt != QSVD_CACHE_F16:
+            self.k_scale = torch.zeros(shape[:3], dtype=torch.float32, device=device)
+            self.v_scale = torch.zeros(shape[:3], dtype=torch.float32, device=device)
+        self.c = QsvdPages(fmt, dtype, n_kv_heads, head_dim, page_size, n_pages, ptr(self.k), ptr(self.v),
+                           ptr(self.k_scale), ptr(self.v_scale))
+
+
+class DevicePageBatch:
+    """What a step brings to every sequence, in device memory; ``.c`` is the
+    qsvd_page_batch struct.  ``lengths`` count the step's new tokens; ``new``
+    are how many those are."""
+
+    def __init__(self, page_table, lengths, new, device="cuda", max_len=None, max_new=None, n_rows=None):
+        import torch
+        lengths, new = list(lengths), list(new)
+        first = [sum(new[:b]) for b in range(len(new) + 1)]
+        self.page_table = torch.as_tensor(page_table, dtype=torch.int32).to(device).contiguous()
+        self.seq_len = torch.tensor(lengths, dtype=torch.int32, device=device)
+        self.first = torch.tensor(first, dtype=torch.int32, device=device)
+        self.n_rows = first[-1] if n_rows is None else n_rows
+        self.c = QsvdPageBatch(len(lengths), self.page_table.shape[1], ptr(self.page_table), ptr(self.seq_len),
+                               ptr(self.first), max(lengths) if max_len is None else max_len,
+                               max(new) if max_new is None else max_new, self.n_rows)
 
 
 def projection_evaluator(n_q_heads, n_kv_heads, head_dim, w_bits=8, w_group=0, a_bits=8):

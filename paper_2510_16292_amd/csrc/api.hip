@@ -647,6 +647,159 @@ qsvd_status qsvd_linear_i8(const void* xq, int64_t ldx, const float* sx, const v
   return hip_status(launch_linear_i8(p, (hipStream_t)stream), "linear_i8");
 }
 
+// ---------------------------------------------------------------- rotary positions, paged cache
+constexpr int32_t kMaxHeads = 256;         // rows of a launch times its heads stay below 2^32 threads
+constexpr int32_t kMaxPageBatch = 65536;
+
+// A row operand of `width` elements per row (checked also where p is NULL).
+static qsvd_status check_head_rows(const char* name, const void* p, int64_t ld, int64_t width) {
+  if (!p) return fail(QSVD_ERR_INVALID_ARG, "%s is NULL", name);
+  if (ld < width)
+    return fail(QSVD_ERR_INVALID_ARG, "row stride of %s %lld < %lld", name, (long long)ld, (long long)width);
+  if (ld % 8 || !aligned(p, 16))
+    return fail(QSVD_ERR_UNSUPPORTED, "%s must be 16-byte aligned with a row stride that is a multiple of 8", name);
+  return QSVD_OK;
+}
+
+static qsvd_status check_rope(const qsvd_rope* r) {
+  if (!r) return fail(QSVD_ERR_INVALID_ARG, "rope is NULL");
+  if (r->head_dim <= 0) return fail(QSVD_ERR_INVALID_ARG, "head_dim must be positive");
+  if (r->n_axes < 1 || r->n_axes > QSVD_ROPE_MAX_AXES)
+    return fail(QSVD_ERR_INVALID_ARG, "n_axes must be 1 to %d", QSVD_ROPE_MAX_AXES);
+  if (r->order != QSVD_ROPE_RUNNING && r->order != QSVD_ROPE_RESTART)
+    return fail(QSVD_ERR_INVALID_ARG, "order must be QSVD_ROPE_RUNNING or QSVD_ROPE_RESTART");
+  if (!(r->theta > 1.f) || isinf(r->theta)) return fail(QSVD_ERR_INVALID_ARG, "theta must be finite and > 1");
+  if (r->head_dim % 16 || r->head_dim > 256)
+    return fail(QSVD_ERR_UNSUPPORTED, "head_dim must be a multiple of 16 up to 256");
+  int64_t pairs = 0;
+  for (int a = 0; a < r->n_axes; ++a) {
+    if (r->section[a] < 0) return fail(QSVD_ERR_INVALID_ARG, "section[%d] is negative", a);
+    pairs += r->section[a];
+  }
+  if (pairs != r->head_dim / 2)
+    return fail(QSVD_ERR_INVALID_ARG, "the sections sum to %lld, not head_dim / 2 = %d", (long long)pairs, r->head_dim / 2);
+  return QSVD_OK;
+}
+
+qsvd_status qsvd_rope_axes(const qsvd_rope* rope, const int32_t* pos, int64_t ldpos, int64_t M, int32_t dtype,
+                           const void* q, int64_t ldq, int32_t n_q_heads, void* q_out, int64_t ldqo, const void* k,
+                           int64_t ldk, int32_t n_k_heads, void* k_out, int64_t ldko, void* stream) {
+  qsvd_status st = check_rope(rope);
+  if (st != QSVD_OK || (st = check_dtype(dtype)) != QSVD_OK) return st;
+  if (M < 0 || n_q_heads <= 0 || n_k_heads < 0)
+    return fail(QSVD_ERR_INVALID_ARG, "bad sizes M=%lld n_q_heads=%d n_k_heads=%d", (long long)M, n_q_heads, n_k_heads);
+  if (!k != !k_out || !k != !n_k_heads)
+    return fail(QSVD_ERR_INVALID_ARG, "k, k_out and n_k_heads are given together or not at all");
+  if (ldpos < M) return fail(QSVD_ERR_INVALID_ARG, "stride of pos %lld < M %lld", (long long)ldpos, (long long)M);
+  if (M > kMaxRows) return fail(QSVD_ERR_UNSUPPORTED, "M must be at most %lld", (long long)kMaxRows);
+  if ((int64_t)n_q_heads + n_k_heads > kMaxHeads)
+    return fail(QSVD_ERR_UNSUPPORTED, "at most %d heads", kMaxHeads);
+  if (M == 0) return QSVD_OK;
+  if (!pos) return fail(QSVD_ERR_INVALID_ARG, "pos is NULL");
+  if (!aligned(pos, 4)) return fail(QSVD_ERR_UNSUPPORTED, "pos must be 4-byte aligned");
+  const int64_t wq = (int64_t)n_q_heads * rope->head_dim, wk = (int64_t)n_k_heads * rope->head_dim;
+  if ((st = check_head_rows("q", q, ldq, wq)) != QSVD_OK || (st = check_head_rows("q_out", q_out, ldqo, wq)) != QSVD_OK)
+    return st;
+  if (k && ((st = check_head_rows("k", k, ldk, wk)) != QSVD_OK || (st = check_head_rows("k_out", k_out, ldko, wk)) != QSVD_OK))
+    return st;
+  if (M > 1 && ((q_out == q && ldqo != ldq) || (k && k_out == k && ldko != ldk)))
+    return fail(QSVD_ERR_INVALID_ARG, "an output in place of its input must have its row stride");
+  const RopeArgs a{pos, ldpos, M, dtype, rope->head_dim, q, ldq, n_q_heads, q_out, ldqo, k, ldk, n_k_heads, k_out, ldko};
+  return hip_status(launch_rope_axes(*rope, a, (hipStream_t)stream), "rope_axes");
+}
+
+static qsvd_status check_pages(const qsvd_pages* p) {
+  if (!p) return fail(QSVD_ERR_INVALID_ARG, "pages is NULL");
+  if (p->fmt < QSVD_CACHE_F16 || p->fmt > QSVD_CACHE_I4) return fail(QSVD_ERR_INVALID_ARG, "unknown cache format");
+  const qsvd_status st = check_dtype(p->dtype);
+  if (st != QSVD_OK) return st;
+  if (p->n_kv_heads <= 0 || p->head_dim <= 0 || p->page_size <= 0 || p->n_pages <= 0)
+    return fail(QSVD_ERR_INVALID_ARG, "page sizes must be positive");
+  if (!p->k || !p->v) return fail(QSVD_ERR_INVALID_ARG, "pages k/v is NULL");
+  if (p->fmt != QSVD_CACHE_F16 && (!p->k_scale || !p->v_scale))
+    return fail(QSVD_ERR_INVALID_ARG, "integer pages need scales");
+  if (p->head_dim != 64 && p->head_dim != 128) return fail(QSVD_ERR_UNSUPPORTED, "head_dim must be 64 or 128");
+  if (p->page_size < 16 || p->page_size > 1024 || (p->page_size & (p->page_size - 1)))
+    return fail(QSVD_ERR_UNSUPPORTED, "page_size must be a power of two, 16 to 1024");
+  if (p->n_kv_heads > kMaxHeads) return fail(QSVD_ERR_UNSUPPORTED, "n_kv_heads must be at most %d", kMaxHeads);
+  if (!aligned(p->k, 16) || !aligned(p->v, 16)) return fail(QSVD_ERR_UNSUPPORTED, "pages must be 16-byte aligned");
+  if (!aligned(p->k_scale, 4) || !aligned(p->v_scale, 4))
+    return fail(QSVD_ERR_UNSUPPORTED, "page scales must be 4-byte aligned");
+  return QSVD_OK;
+}
+
+static qsvd_status check_page_batch(const qsvd_page_batch* b) {
+  if (!b) return fail(QSVD_ERR_INVALID_ARG, "batch is NULL");
+  if (b->batch <= 0 || b->max_pages <= 0) return fail(QSVD_ERR_INVALID_ARG, "batch and max_pages must be positive");
+  if (!b->page_table || !b->seq_len || !b->first)
+    return fail(QSVD_ERR_INVALID_ARG, "page_table, seq_len or first is NULL");
+  if (b->max_len < 0 || b->max_new < 0 || b->n_rows < 0)
+    return fail(QSVD_ERR_INVALID_ARG, "max_len, max_new and n_rows must not be negative");
+  if (b->batch > kMaxPageBatch) return fail(QSVD_ERR_UNSUPPORTED, "batch must be at most %d", kMaxPageBatch);
+  if (b->n_rows > kMaxRows) return fail(QSVD_ERR_UNSUPPORTED, "n_rows must be at most %lld", (long long)kMaxRows);
+  if (!aligned(b->page_table, 4) || !aligned(b->seq_len, 4) || !aligned(b->first, 4))
+    return fail(QSVD_ERR_UNSUPPORTED, "page_table, seq_len and first must be 4-byte aligned");
+  return QSVD_OK;
+}
+
+static int32_t page_bits(const qsvd_pages& p) { return __builtin_ctz((unsigned)p.page_size); }
+
+static qsvd_status paged_rows(const qsvd_pages* pages, const qsvd_page_batch* batch, void* k, int64_t ldk, void* v,
+                              int64_t ldv, float clip, bool read, void* stream) {
+  qsvd_status st = check_pages(pages);
+  if (st != QSVD_OK || (st = check_page_batch(batch)) != QSVD_OK) return st;
+  if (!(clip > 0.f && clip <= 1.f)) return fail(QSVD_ERR_INVALID_ARG, "clip must be in (0, 1]");
+  if (batch->n_rows == 0) return QSVD_OK;
+  const int64_t w = (int64_t)pages->n_kv_heads * pages->head_dim;
+  if ((st = check_head_rows("k", k, ldk, w)) != QSVD_OK || (st = check_head_rows("v", v, ldv, w)) != QSVD_OK) return st;
+  const PagedRowsArgs a{*pages, *batch, page_bits(*pages), k, ldk, v, ldv, clip};
+  return hip_status(launch_paged_rows(a, read, (hipStream_t)stream), read ? "paged_read" : "paged_append");
+}
+
+qsvd_status qsvd_paged_append(const qsvd_pages* pages, const qsvd_page_batch* batch, const void* k, int64_t ldk,
+                              const void* v, int64_t ldv, float clip, void* stream) {
+  return paged_rows(pages, batch, (void*)k, ldk, (void*)v, ldv, clip, false, stream);
+}
+
+qsvd_status qsvd_paged_read(const qsvd_pages* pages, const qsvd_page_batch* batch, void* k, int64_t ldk, void* v,
+                            int64_t ldv, void* stream) {
+  return paged_rows(pages, batch, k, ldk, v, ldv, 1.f, true, stream);
+}
+
+static qsvd_status check_query_heads(const qsvd_pages& p, int32_t n_q_heads) {
+  if (n_q_heads <= 0 || n_q_heads % p.n_kv_heads)
+    return fail(QSVD_ERR_INVALID_ARG, "n_q_heads (%d) must be a multiple of n_kv_heads (%d)", n_q_heads, p.n_kv_heads);
+  if (n_q_heads > kMaxHeads) return fail(QSVD_ERR_UNSUPPORTED, "n_q_heads must be at most %d", kMaxHeads);
+  return QSVD_OK;
+}
+
+size_t qsvd_paged_attention_workspace_size(const qsvd_pages* pages, const qsvd_page_batch* batch, int32_t n_q_heads) {
+  if (check_pages(pages) != QSVD_OK || check_page_batch(batch) != QSVD_OK || check_query_heads(*pages, n_q_heads) != QSVD_OK)
+    return 0;
+  return paged_attention_workspace(*pages, *batch, n_q_heads);
+}
+
+qsvd_status qsvd_paged_attention(const qsvd_pages* pages, const qsvd_page_batch* batch, const void* q, int64_t ldq,
+                                 int32_t n_q_heads, float sm_scale, void* out, int64_t ldo, void* ws, size_t ws_bytes,
+                                 void* stream) {
+  qsvd_status st = check_pages(pages);
+  if (st != QSVD_OK || (st = check_page_batch(batch)) != QSVD_OK || (st = check_query_heads(*pages, n_q_heads)) != QSVD_OK)
+    return st;
+  if (!(sm_scale >= 0.f) || isinf(sm_scale)) return fail(QSVD_ERR_INVALID_ARG, "sm_scale must be finite and >= 0");
+  if (batch->n_rows == 0) return QSVD_OK;
+  const int64_t w = (int64_t)n_q_heads * pages->head_dim;
+  if ((st = check_head_rows("q", q, ldq, w)) != QSVD_OK || (st = check_head_rows("out", out, ldo, w)) != QSVD_OK) return st;
+  const size_t need = paged_attention_workspace(*pages, *batch, n_q_heads);
+  if (need > 0) {
+    if (!ws || ws_bytes < need)
+      return fail(QSVD_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", ws ? ws_bytes : (size_t)0, need);
+    if (!aligned(ws, 16)) return fail(QSVD_ERR_UNSUPPORTED, "ws must be 16-byte aligned");
+  }
+  const PagedAttnArgs a{*pages, *batch, page_bits(*pages), q, ldq, n_q_heads,
+                        sm_scale > 0.f ? sm_scale : 1.f / sqrtf((float)pages->head_dim), out, ldo};
+  return hip_status(launch_paged_attention(a, ws, (hipStream_t)stream), "paged_attention");
+}
+
 qsvd_status qsvd_profile_enable(int32_t on, const char* filter) {
   std::lock_guard<std::mutex> lk(g_prof_mu);
   g_prof_on = on != 0;

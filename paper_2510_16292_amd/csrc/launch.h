@@ -230,4 +230,49 @@ struct LinearArgs {
 };
 hipError_t launch_linear_i8(const LinearArgs& p, hipStream_t s);
 
+// Rotary embedding at positions with several axes (k NULL: n_k is 0).
+struct RopeArgs {
+  const int32_t* pos;       // [axes][ldpos]
+  int64_t ldpos, M;
+  int32_t dtype, head_dim;
+  const void* q;
+  int64_t ldq;
+  int32_t n_q;
+  void* q_out;
+  int64_t ldqo;
+  const void* k;
+  int64_t ldk;
+  int32_t n_k;
+  void* k_out;
+  int64_t ldko;
+};
+hipError_t launch_rope_axes(const qsvd_rope& r, const RopeArgs& a, hipStream_t s);
+
+// Rows into the pages of a key/value cache (k, v are read) or out of them.
+struct PagedRowsArgs {
+  qsvd_pages pages;
+  qsvd_page_batch batch;
+  int32_t page_bits;        // page_size = 1 << page_bits
+  void* k;
+  int64_t ldk;
+  void* v;
+  int64_t ldv;
+  float clip;
+};
+hipError_t launch_paged_rows(const PagedRowsArgs& a, bool read, hipStream_t s);
+
+struct PagedAttnArgs {
+  qsvd_pages pages;
+  qsvd_page_batch batch;
+  int32_t page_bits;
+  const void* q;
+  int64_t ldq;
+  int32_t n_q_heads;
+  float sm_scale;
+  void* out;
+  int64_t ldo;
+};
+size_t paged_attention_workspace(const qsvd_pages& p, const qsvd_page_batch& b, int32_t n_q_heads);
+hipError_t launch_paged_attention(const PagedAttnArgs& a, void* ws, hipStream_t s);
+
 }  // namespace qsvd

@@ -1,0 +1,57 @@
+// What the kernels over a paged key/value cache share: where a row is.
+#pragma once
+#include "common.h"
+
+namespace qsvd {
+
+// How many of first[1 .. batch] are at most m, counted by the `width` lanes
+// (a power of two) of a lane's group, all of which receive it: the sequence
+// that row m is of, or batch if the row is behind the last one.
+__device__ __forceinline__ int page_sequence(const int32_t* __restrict__ first, int batch, int64_t m, int lane, int width) {
+  int n = 0;
+  for (int i = 1 + (lane & (width - 1)); i <= batch; i += width) n += first[i] <= m;
+  for (int o = width >> 1; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
+  return n;
+}
+
+// The page of position pos of sequence b, or -1 where it has no place.
+__device__ __forceinline__ int page_of(const qsvd_page_batch& t, int n_pages, int page_bits, int b, int pos) {
+  const int col = pos >> page_bits;          // (negative for a negative position)
+  if (pos < 0 || col >= t.max_pages) return -1;
+  const int p = t.page_table[(int64_t)b * t.max_pages + col];
+  return p >= 0 && p < n_pages ? p : -1;
+}
+
+// Codes of fp32 values that came from 16 bits: the integer nearest to x qm / a,
+// ties to even, a = clip * max |x| over the row.  A quotient half way between
+// two integers has to come out as exactly that, which x * (qm / a) does not
+// do; so the quotient is corrected once by its remainder: t = x qm 2^-e is
+// exact (24 bits), a 2^-e lies in [1, 2), and q0 + (t - q0 a) / a is off by
+// 2^-46 before its own rounding, which keeps halves (no quotient of 16-bit
+// values other than a half comes as near to one as that).
+struct RowCode {
+  float s, up, inv, a;        // scale; qm 2^-e; 1 / (a 2^-e), 0: codes 0; a 2^-e
+};
+__device__ __forceinline__ RowCode row_code(float amax, float clip, float qm) {
+  RowCode r;
+  const float a = mul_rn(clip, amax);
+  r.s = div_rn(a, qm);
+  if (!(a <= 3.4028234663852886e38f)) return RowCode{__uint_as_float(0x7fc00000u), 0.f, 0.f, 1.f};   // infinite or NaN
+  if (a < 1.504632769052528e-36f) return RowCode{1.f, 0.f, 0.f, 1.f};      // 2^-119
+  const int e = (int)(__float_as_uint(a) >> 23) - 127;
+  r.a = __uint_as_float((__float_as_uint(a) & 0x007fffffu) | 0x3f800000u);
+  r.up = ldexpf(qm, -e);
+  r.inv = div_rn(1.f, r.a);
+  return r;
+}
+// The low byte (nibble) of the word is the code.  fmed3 and the addition of
+// 1.5 * 2^23 clamp and round half to even (code_bits says how); a NaN element
+// belongs to a row whose `inv` and `up` are 0, and is made 0 first.
+__device__ __forceinline__ uint32_t row_code_bits(float x, const RowCode& r, float qm) {
+  const float t = r.up == 0.f ? 0.f : mul_rn(x, r.up);
+  const float q0 = mul_rn(t, r.inv);
+  const float q = fmaf(fmaf(-q0, r.a, t), r.inv, q0);
+  return __float_as_uint(add_rn(__builtin_amdgcn_fmed3f(q, -qm, qm), 12582912.0f));
+}
+
+}  // namespace qsvd

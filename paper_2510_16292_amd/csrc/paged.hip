@@ -1,0 +1,140 @@
+// New key and value rows into the pages of a cache, and rows back out of it.
+//
+// A row's head vector is dh elements; dh / 8 lanes hold it, eight elements
+// each, for the key and the value at once.  Per head vector: a = clip max |x|,
+// scale a / Qm, codes rint(x Qm / a) (paged.h); 16-bit pages take the elements
+// as they are.  A workgroup has kPagedRows consecutive rows of one head: their
+// places in a page follow each other, so that its stores fill whole lines also
+// where a row of codes is half of one.
+//
+// What bounds it: memory, each row read once and each code written once; for a
+// decode step's few rows the chain of loads that finds a row's place (first,
+// seq_len, page_table), which the row's own loads are issued before.
+#include <algorithm>
+
+#include "elem16.h"
+#include "launch.h"
+#include "paged.h"
+
+namespace qsvd {
+
+// max |x|, or NaN if either is NaN
+__device__ __forceinline__ float paged_max(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
+template <int DH>
+__device__ __forceinline__ float head_max(float v) {
+#pragma unroll
+  for (int o = DH / 16; o > 0; o >>= 1) v = paged_max(v, __shfl_xor(v, o, 64));
+  return v;
+}
+
+template <bool BF, int DH, int FMT>
+__device__ __forceinline__ void store_head(const i32x4& x, void* pool, float* scales, int64_t row, int c, float clip) {
+  using E = Elem16<BF>;
+  if constexpr (FMT == QSVD_CACHE_F16) {
+    reinterpret_cast<i32x4*>(pool)[row * (DH / 8) + c] = x;
+  } else {
+    constexpr float qm = FMT == QSVD_CACHE_I8 ? 127.f : 7.f;
+    float f[8];
+    E::unpack(x, f);
+    float amax = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) amax = paged_max(amax, fabsf(f[e]));
+    const RowCode r = row_code(head_max<DH>(amax), clip, qm);
+    uint32_t b[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) b[e] = row_code_bits(f[e], r, qm);
+    if (row < 0) return;
+    if (FMT == QSVD_CACHE_I8) {
+      const uint2 w = make_uint2(pack4_codes8(b[0], b[1], b[2], b[3]), pack4_codes8(b[4], b[5], b[6], b[7]));
+      reinterpret_cast<uint2*>(pool)[row * (DH / 8) + c] = w;
+    } else {
+      reinterpret_cast<uint32_t*>(pool)[row * (DH / 8) + c] = pack8_codes4(b);
+    }
+    if (c == 0) scales[row] = r.s;
+  }
+}
+
+template <bool BF, int DH, int FMT>
+__device__ __forceinline__ i32x4 load_head(const void* pool, const float* scales, int64_t row, int c) {
+  using E = Elem16<BF>;
+  if (row < 0) return i32x4{0, 0, 0, 0};
+  if constexpr (FMT == QSVD_CACHE_F16) {
+    return reinterpret_cast<const i32x4*>(pool)[row * (DH / 8) + c];
+  } else {
+    float f[8];
+    const float s = scales[row];
+    if (FMT == QSVD_CACHE_I8) {
+      const uint2 w = reinterpret_cast<const uint2*>(pool)[row * (DH / 8) + c];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] = mul_rn((float)(int8_t)((e < 4 ? w.x : w.y) >> (8 * (e & 3))), s);
+    } else {
+      const uint32_t w = reinterpret_cast<const uint32_t*>(pool)[row * (DH / 8) + c];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] = mul_rn((float)((int)(w << (28 - 4 * e)) >> 28), s);
+    }
+    return E::pack(f);
+  }
+}
+
+constexpr int kPagedThreads = 256;
+
+template <bool BF, int DH, int FMT, bool READ>
+__global__ void __launch_bounds__(kPagedThreads)
+paged_rows_kernel(PagedRowsArgs a) {
+  constexpr int LPR = DH / 8;                       // lanes of a head vector
+  const int lane = threadIdx.x & 63, c = threadIdx.x % LPR, h = blockIdx.y;
+  const int64_t m = (int64_t)blockIdx.x * (kPagedThreads / LPR) + threadIdx.x / LPR;
+  i32x4 kx{}, vx{};
+  uint16_t* kp = (uint16_t*)a.k + m * a.ldk + h * DH + 8 * c;
+  uint16_t* vp = (uint16_t*)a.v + m * a.ldv + h * DH + 8 * c;
+  const bool row = m < a.batch.n_rows;
+  if (!READ && row) {
+    kx = *reinterpret_cast<const i32x4*>(kp);
+    vx = *reinterpret_cast<const i32x4*>(vp);
+  }
+  const int b = page_sequence(a.batch.first, a.batch.batch, m, lane, LPR);
+  const bool live = row && b < a.batch.batch;
+  int64_t at = -1;                                  // the head vector's row in the pool
+  if (live) {
+    const int pos = a.batch.seq_len[b] - (int)(a.batch.first[b + 1] - m);
+    const int page = page_of(a.batch, a.pages.n_pages, a.page_bits, b, pos);
+    if (page >= 0)
+      at = (((int64_t)page * a.pages.n_kv_heads + h) << a.page_bits) + (pos & (a.pages.page_size - 1));
+  }
+  if constexpr (READ) {
+    if (!live) return;
+    *reinterpret_cast<i32x4*>(kp) = load_head<BF, DH, FMT>(a.pages.k, a.pages.k_scale, at, c);
+    *reinterpret_cast<i32x4*>(vp) = load_head<BF, DH, FMT>(a.pages.v, a.pages.v_scale, at, c);
+  } else {
+    if (FMT == QSVD_CACHE_F16 && at < 0) return;    // (codes: every lane takes part in the row's maximum)
+    store_head<BF, DH, FMT>(kx, a.pages.k, a.pages.k_scale, at, c, a.clip);
+    store_head<BF, DH, FMT>(vx, a.pages.v, a.pages.v_scale, at, c, a.clip);
+  }
+}
+
+template <bool BF, int DH, int FMT>
+static hipError_t launch_rows(const PagedRowsArgs& a, bool read, hipStream_t s) {
+  constexpr int rows = kPagedThreads / (DH / 8);
+  const dim3 grid((unsigned)((a.batch.n_rows + rows - 1) / rows), (unsigned)a.pages.n_kv_heads);
+  KernelScope ks(read ? "paged_read" : "paged_append", s);
+  auto kern = read ? paged_rows_kernel<BF, DH, FMT, true> : paged_rows_kernel<BF, DH, FMT, false>;
+  QSVD_LAUNCH(ks, kern, grid, dim3(kPagedThreads), 0, s, a);
+  return hipGetLastError();
+}
+
+template <bool BF, int DH>
+static hipError_t launch_rows(const PagedRowsArgs& a, bool read, hipStream_t s) {
+  return a.pages.fmt == QSVD_CACHE_I8   ? launch_rows<BF, DH, QSVD_CACHE_I8>(a, read, s)
+         : a.pages.fmt == QSVD_CACHE_I4 ? launch_rows<BF, DH, QSVD_CACHE_I4>(a, read, s)
+                                        : launch_rows<BF, DH, QSVD_CACHE_F16>(a, read, s);
+}
+
+hipError_t launch_paged_rows(const PagedRowsArgs& a, bool read, hipStream_t s) {
+  if (a.batch.n_rows == 0) return hipSuccess;
+  const bool bf = a.pages.dtype == QSVD_BF16;
+  if (a.pages.head_dim == 128) return bf ? launch_rows<true, 128>(a, read, s) : launch_rows<false, 128>(a, read, s);
+  return bf ? launch_rows<true, 64>(a, read, s) : launch_rows<false, 64>(a, read, s);
+}
+
+}  // namespace qsvd
