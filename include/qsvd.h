@@ -514,7 +514,7 @@ qsvd_status qsvd_paged_read(const qsvd_pages* pages, const qsvd_page_batch* batc
  * device: a captured call may be replayed with other lengths up to max_len and
  * max_new.  A call repeats exactly for the same arguments.
  * Requires n_q_heads a multiple of n_kv_heads and at most 256, batch <= 65536,
- * n_rows < 2^22, 16-byte aligned rows, pages and ws. */
+ * batch * n_kv_heads <= 2^18, n_rows < 2^22, 16-byte aligned rows, pages and ws. */
 qsvd_status qsvd_paged_attention(const qsvd_pages* pages, const qsvd_page_batch* batch, const void* q, int64_t ldq,
                                  int32_t n_q_heads, float sm_scale, void* out, int64_t ldo, void* ws, size_t ws_bytes,
                                  void* stream);

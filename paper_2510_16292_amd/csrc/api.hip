@@ -650,6 +650,7 @@ qsvd_status qsvd_linear_i8(const void* xq, int64_t ldx, const float* sx, const v
 // ---------------------------------------------------------------- rotary positions, paged cache
 constexpr int32_t kMaxHeads = 256;         // rows of a launch times its heads stay below 2^32 threads
 constexpr int32_t kMaxPageBatch = 65536;
+constexpr int64_t kMaxPageGroups = (int64_t)1 << 18;      // sequences times key/value heads: 64 rows of each are workgroups
 
 // A row operand of `width` elements per row (checked also where p is NULL).
 static qsvd_status check_head_rows(const char* name, const void* p, int64_t ld, int64_t width) {
@@ -766,15 +767,17 @@ qsvd_status qsvd_paged_read(const qsvd_pages* pages, const qsvd_page_batch* batc
   return paged_rows(pages, batch, k, ldk, v, ldv, 1.f, true, stream);
 }
 
-static qsvd_status check_query_heads(const qsvd_pages& p, int32_t n_q_heads) {
+static qsvd_status check_query_heads(const qsvd_pages& p, int32_t batch, int32_t n_q_heads) {
   if (n_q_heads <= 0 || n_q_heads % p.n_kv_heads)
     return fail(QSVD_ERR_INVALID_ARG, "n_q_heads (%d) must be a multiple of n_kv_heads (%d)", n_q_heads, p.n_kv_heads);
   if (n_q_heads > kMaxHeads) return fail(QSVD_ERR_UNSUPPORTED, "n_q_heads must be at most %d", kMaxHeads);
+  if ((int64_t)batch * p.n_kv_heads > kMaxPageGroups)
+    return fail(QSVD_ERR_UNSUPPORTED, "batch * n_kv_heads must be at most %lld", (long long)kMaxPageGroups);
   return QSVD_OK;
 }
 
 size_t qsvd_paged_attention_workspace_size(const qsvd_pages* pages, const qsvd_page_batch* batch, int32_t n_q_heads) {
-  if (check_pages(pages) != QSVD_OK || check_page_batch(batch) != QSVD_OK || check_query_heads(*pages, n_q_heads) != QSVD_OK)
+  if (check_pages(pages) != QSVD_OK || check_page_batch(batch) != QSVD_OK || check_query_heads(*pages, batch->batch, n_q_heads) != QSVD_OK)
     return 0;
   return paged_attention_workspace(*pages, *batch, n_q_heads);
 }
@@ -783,7 +786,7 @@ qsvd_status qsvd_paged_attention(const qsvd_pages* pages, const qsvd_page_batch*
                                  int32_t n_q_heads, float sm_scale, void* out, int64_t ldo, void* ws, size_t ws_bytes,
                                  void* stream) {
   qsvd_status st = check_pages(pages);
-  if (st != QSVD_OK || (st = check_page_batch(batch)) != QSVD_OK || (st = check_query_heads(*pages, n_q_heads)) != QSVD_OK)
+  if (st != QSVD_OK || (st = check_page_batch(batch)) != QSVD_OK || (st = check_query_heads(*pages, batch->batch, n_q_heads)) != QSVD_OK)
     return st;
   if (!(sm_scale >= 0.f) || isinf(sm_scale)) return fail(QSVD_ERR_INVALID_ARG, "sm_scale must be finite and >= 0");
   if (batch->n_rows == 0) return QSVD_OK;

@@ -1,0 +1,137 @@
+// What the kernels of the attention over a paged key/value cache share.
+#pragma once
+#include "elem16.h"
+#include "flash.h"
+#include "launch.h"
+#include "paged.h"
+
+namespace qsvd {
+
+typedef __attribute__((address_space(3))) uint8_t lds_byte;
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+
+// The products' element type: bf16 over pages of bf16 rows, else fp16 (integer
+// codes are exact in it, and a query is brought into its range by a power of
+// two).
+template <bool BF>
+struct Mat16 {
+  using X8 = f16x8;
+  using X4 = f16x4;
+  static __device__ __forceinline__ f32x4 mfma16(X8 a, X8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+  static __device__ __forceinline__ f32x16 mfma32(X8 a, X8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+};
+template <>
+struct Mat16<true> {
+  using X8 = bf16x8;
+  using X4 = bf16x4;
+  static __device__ __forceinline__ f32x4 mfma16(X8 a, X8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+  static __device__ __forceinline__ f32x16 mfma32(X8 a, X8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+};
+
+// Four int8 codes of a word as fp16: with its sign bit turned a code is 128
+// more and unsigned, the low mantissa bits of 1024 + code + 128.
+__device__ __forceinline__ void widen_i8(uint32_t w, f16x2& lo, f16x2& hi) {
+  const uint32_t u = w ^ 0x80808080u, k = 0x64646464u;
+  const f16x2 bias = {(_Float16)1152.f, (_Float16)1152.f};
+  lo = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(k, u, 0x04010400u)) - bias;
+  hi = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(k, u, 0x04030402u)) - bias;
+}
+__device__ __forceinline__ f16x8 widen_i8x8(uint32_t w0, uint32_t w1) {
+  f16x2 a, b, c, d;
+  widen_i8(w0, a, b);
+  widen_i8(w1, c, d);
+  return f16x8{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
+}
+// Four bytes of signed nibbles (the low one of each byte) as fp16.
+__device__ __forceinline__ void widen_i4_bytes(uint32_t w, f16x2& lo, f16x2& hi) {
+  const uint32_t u = (w & 0x0f0f0f0fu) ^ 0x08080808u, k = 0x64646464u;
+  const f16x2 bias = {(_Float16)1032.f, (_Float16)1032.f};
+  lo = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(k, u, 0x04010400u)) - bias;
+  hi = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(k, u, 0x04030402u)) - bias;
+}
+__device__ __forceinline__ f16x8 widen_i4x8_bytes(uint32_t w0, uint32_t w1) {
+  f16x2 a, b, c, d;
+  widen_i4_bytes(w0, a, b);
+  widen_i4_bytes(w1, c, d);
+  return f16x8{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
+}
+// Eight nibbles of a word as fp16, in the order kNibbleOrder.
+__device__ __forceinline__ f16x8 widen_i4x8(uint32_t w) {
+  const uint32_t u = w ^ 0x88888888u;
+  const f16x2 bias = {(_Float16)1032.f, (_Float16)1032.f};
+  f16x2 p[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) p[j] = __builtin_bit_cast(f16x2, ((u >> (4 * j)) & 0x000f000fu) | 0x64006400u) - bias;
+  return f16x8{p[0].x, p[0].y, p[1].x, p[1].y, p[2].x, p[2].y, p[3].x, p[3].y};
+}
+template <class X8>
+__device__ __forceinline__ X8 nibble_order(X8 x) {
+  return __builtin_shufflevector(x, x, 0, 4, 1, 5, 2, 6, 3, 7);
+}
+
+// Two 16-bit elements with 0 in the place of infinities and NaN.
+template <bool BF>
+__device__ __forceinline__ uint32_t finite16(uint32_t x) {
+  constexpr uint32_t ex = BF ? 0x7f80u : 0x7c00u;
+  const uint32_t lo = (x & ex) == ex ? 0u : x & 0xffffu, hi = (x & ex << 16) == ex << 16 ? 0u : x & 0xffff0000u;
+  return lo | hi;
+}
+
+// Direct loads into LDS, lane p's bytes to lds + (bytes a lane) p (`lds`
+// wave-uniform): flash.hip says why they are asm.  They complete in order; the
+// wave waits for them with vmcnt.
+__device__ __forceinline__ void direct_load16(const void* base, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory");
+}
+__device__ __forceinline__ void direct_load16(const void* p, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(p) : "memory");
+}
+__device__ __forceinline__ void direct_load4(const void* p, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(p) : "memory");
+}
+
+// A sequence of the step: its rows and what its queries may see.
+struct PageSeq {
+  int n_new;        // new tokens; 0: none
+  int row0;         // first row
+  int len;          // tokens, the new ones included
+  int kend;         // keys: len, but at most what the table has places for
+};
+__device__ __forceinline__ PageSeq page_seq(const qsvd_page_batch& t, int page_bits, int b) {
+  PageSeq s;
+  s.row0 = t.first[b];
+  s.n_new = t.first[b + 1] - s.row0;
+  s.len = t.seq_len[b];
+  s.kend = (int)min((int64_t)s.len, (int64_t)t.max_pages << page_bits);
+  return s;
+}
+
+// How the keys of a sequence are shared out: `parts` workgroups, part p of them
+// taking the tiles [p T / parts, (p + 1) T / parts).
+struct PagedPlan {
+  int few;              // a sequence of at most so many rows per key/value head is the decode kernel's (16 or 32), 0: none is
+  int decode_parts, chunk_parts;      // most parts of either kernel (1: outputs are written directly)
+  int64_t decode_rows;  // rows of one part in the workspace: batch * n_kv_heads * few
+  int64_t chunk_rows;   // n_rows * n_q_heads
+  int64_t rows() const { return decode_parts_rows() + chunk_parts_rows(); }
+  int64_t decode_parts_rows() const { return decode_parts > 1 ? decode_parts * decode_rows : 0; }
+  int64_t chunk_parts_rows() const { return chunk_parts > 1 ? chunk_parts * chunk_rows : 0; }
+};
+constexpr int kDecodeTile = 32;       // keys of a wave's tile
+constexpr int kDecodeWaves = 4;
+constexpr int kDecodeMinTiles = 8;    // ... of a part
+__device__ __forceinline__ int decode_parts(const PagedPlan& p, int kend) {
+  const int tiles = (max(kend, 0) + kDecodeTile - 1) / kDecodeTile;
+  return max(1, min(p.decode_parts, tiles / kDecodeMinTiles));
+}
+
+// Workspace: fp32 rows [rows][head_dim], then (m, l) of each.
+struct PagedPartial {
+  float* o;
+  float2* ml;
+};
+
+hipError_t launch_paged_decode(const PagedAttnArgs& a, const PagedPlan& p, const PagedPartial& ws, hipStream_t s);
+
+}  // namespace qsvd
