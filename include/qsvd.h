@@ -489,8 +489,8 @@ typedef struct {
  *   k, v  device [n_rows][ldk], [n_rows][ldv], heads next to each other
  * Lengths and tables are not changed: the caller advances seq_len before the
  * step, once for all layers.  If two rows have the same place, either may stay.
- * Requires n_kv_heads <= 256, n_rows < 2^22, batch <= 65536, 16-byte aligned
- * rows and pages, 0 < clip <= 1. */
+ * Requires n_kv_heads <= 256, n_rows and max_new < 2^22, batch <= 65536, max_len
+ * <= 2^30, 16-byte aligned rows and pages, 0 < clip <= 1. */
 qsvd_status qsvd_paged_append(const qsvd_pages* pages, const qsvd_page_batch* batch, const void* k, int64_t ldk,
                               const void* v, int64_t ldv, float clip, void* stream);
 
@@ -514,7 +514,9 @@ qsvd_status qsvd_paged_read(const qsvd_pages* pages, const qsvd_page_batch* batc
  * device: a captured call may be replayed with other lengths up to max_len and
  * max_new.  A call repeats exactly for the same arguments.
  * Requires n_q_heads a multiple of n_kv_heads and at most 256, batch <= 65536,
- * batch * n_kv_heads <= 2^18, n_rows < 2^22, 16-byte aligned rows, pages and ws. */
+ * batch * n_kv_heads <= 2^18, batch * n_kv_heads * ceil(max_new * (n_q_heads /
+ * n_kv_heads) / 128) <= 2^22, max_len <= 2^30, n_rows and max_new < 2^22,
+ * 16-byte aligned rows, pages and ws. */
 qsvd_status qsvd_paged_attention(const qsvd_pages* pages, const qsvd_page_batch* batch, const void* q, int64_t ldq,
                                  int32_t n_q_heads, float sm_scale, void* out, int64_t ldo, void* ws, size_t ws_bytes,
                                  void* stream);

@@ -16,7 +16,7 @@ LIB = os.path.join(LIB_DIR, "libqsvd.so")
 
 SOURCES = ["api.hip", "quant.hip", "gemm_i8.hip", "gemm_q4.hip", "skinny.hip", "cache.hip", "attn.hip", "flash.hip",
            "flash_short.hip", "rows.hip", "linear.hip",
-           "rope.hip", "paged.hip", "paged_decode.hip", "paged_attn.hip"]
+           "rope.hip", "paged.hip", "paged_decode.hip", "paged_chunk.hip", "paged_attn.hip"]
 
 # -ffp-contract=off: the quantizer and the dequantization epilogues are defined
 # by separately rounded fp32 operations; explicit fmaf() stays fused.

@@ -650,7 +650,9 @@ qsvd_status qsvd_linear_i8(const void* xq, int64_t ldx, const float* sx, const v
 // ---------------------------------------------------------------- rotary positions, paged cache
 constexpr int32_t kMaxHeads = 256;         // rows of a launch times its heads stay below 2^32 threads
 constexpr int32_t kMaxPageBatch = 65536;
-constexpr int64_t kMaxPageGroups = (int64_t)1 << 18;      // sequences times key/value heads: 64 rows of each are workgroups
+constexpr int32_t kMaxPageLen = 1 << 30;
+constexpr int64_t kMaxPageGroups = (int64_t)1 << 18;      // sequences times key/value heads: 32 rows of each are workgroups
+constexpr int64_t kMaxPageBlocks = (int64_t)1 << 22;      // ... times 128-row blocks of queries
 
 // A row operand of `width` elements per row (checked also where p is NULL).
 static qsvd_status check_head_rows(const char* name, const void* p, int64_t ld, int64_t width) {
@@ -736,6 +738,8 @@ static qsvd_status check_page_batch(const qsvd_page_batch* b) {
     return fail(QSVD_ERR_INVALID_ARG, "page_table, seq_len or first is NULL");
   if (b->max_len < 0 || b->max_new < 0 || b->n_rows < 0)
     return fail(QSVD_ERR_INVALID_ARG, "max_len, max_new and n_rows must not be negative");
+  if (b->max_len > kMaxPageLen) return fail(QSVD_ERR_UNSUPPORTED, "max_len must be at most %d", kMaxPageLen);
+  if (b->max_new > kMaxRows) return fail(QSVD_ERR_UNSUPPORTED, "max_new must be at most %lld", (long long)kMaxRows);
   if (b->batch > kMaxPageBatch) return fail(QSVD_ERR_UNSUPPORTED, "batch must be at most %d", kMaxPageBatch);
   if (b->n_rows > kMaxRows) return fail(QSVD_ERR_UNSUPPORTED, "n_rows must be at most %lld", (long long)kMaxRows);
   if (!aligned(b->page_table, 4) || !aligned(b->seq_len, 4) || !aligned(b->first, 4))
@@ -767,17 +771,21 @@ qsvd_status qsvd_paged_read(const qsvd_pages* pages, const qsvd_page_batch* batc
   return paged_rows(pages, batch, k, ldk, v, ldv, 1.f, true, stream);
 }
 
-static qsvd_status check_query_heads(const qsvd_pages& p, int32_t batch, int32_t n_q_heads) {
+static qsvd_status check_query_heads(const qsvd_pages& p, const qsvd_page_batch& b, int32_t n_q_heads) {
   if (n_q_heads <= 0 || n_q_heads % p.n_kv_heads)
     return fail(QSVD_ERR_INVALID_ARG, "n_q_heads (%d) must be a multiple of n_kv_heads (%d)", n_q_heads, p.n_kv_heads);
   if (n_q_heads > kMaxHeads) return fail(QSVD_ERR_UNSUPPORTED, "n_q_heads must be at most %d", kMaxHeads);
-  if ((int64_t)batch * p.n_kv_heads > kMaxPageGroups)
+  const int64_t groups = (int64_t)b.batch * p.n_kv_heads;
+  if (groups > kMaxPageGroups)
     return fail(QSVD_ERR_UNSUPPORTED, "batch * n_kv_heads must be at most %lld", (long long)kMaxPageGroups);
+  if (groups * (((int64_t)b.max_new * (n_q_heads / p.n_kv_heads) + 127) / 128) > kMaxPageBlocks)
+    return fail(QSVD_ERR_UNSUPPORTED, "batch * n_kv_heads * ceil(max_new * (n_q_heads / n_kv_heads) / 128) must be at most %lld",
+                (long long)kMaxPageBlocks);
   return QSVD_OK;
 }
 
 size_t qsvd_paged_attention_workspace_size(const qsvd_pages* pages, const qsvd_page_batch* batch, int32_t n_q_heads) {
-  if (check_pages(pages) != QSVD_OK || check_page_batch(batch) != QSVD_OK || check_query_heads(*pages, batch->batch, n_q_heads) != QSVD_OK)
+  if (check_pages(pages) != QSVD_OK || check_page_batch(batch) != QSVD_OK || check_query_heads(*pages, *batch, n_q_heads) != QSVD_OK)
     return 0;
   return paged_attention_workspace(*pages, *batch, n_q_heads);
 }
@@ -786,7 +794,7 @@ qsvd_status qsvd_paged_attention(const qsvd_pages* pages, const qsvd_page_batch*
                                  int32_t n_q_heads, float sm_scale, void* out, int64_t ldo, void* ws, size_t ws_bytes,
                                  void* stream) {
   qsvd_status st = check_pages(pages);
-  if (st != QSVD_OK || (st = check_page_batch(batch)) != QSVD_OK || (st = check_query_heads(*pages, batch->batch, n_q_heads)) != QSVD_OK)
+  if (st != QSVD_OK || (st = check_page_batch(batch)) != QSVD_OK || (st = check_query_heads(*pages, *batch, n_q_heads)) != QSVD_OK)
     return st;
   if (!(sm_scale >= 0.f) || isinf(sm_scale)) return fail(QSVD_ERR_INVALID_ARG, "sm_scale must be finite and >= 0");
   if (batch->n_rows == 0) return QSVD_OK;

@@ -91,6 +91,8 @@ __device__ __forceinline__ void direct_load4(const void* p, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(p) : "memory");
 }
 
+constexpr int kMaxKeys = 1 << 30;     // of a sequence: a tile's end fits an int
+
 // A sequence of the step: its rows and what its queries may see.
 struct PageSeq {
   int n_new;        // new tokens; 0: none
@@ -103,19 +105,19 @@ __device__ __forceinline__ PageSeq page_seq(const qsvd_page_batch& t, int page_b
   s.row0 = t.first[b];
   s.n_new = t.first[b + 1] - s.row0;
   s.len = t.seq_len[b];
-  s.kend = (int)min((int64_t)s.len, (int64_t)t.max_pages << page_bits);
+  s.kend = (int)min((int64_t)min(s.len, kMaxKeys), (int64_t)t.max_pages << page_bits);
   return s;
 }
 
 // How the keys of a sequence are shared out: `parts` workgroups, part p of them
 // taking the tiles [p T / parts, (p + 1) T / parts).
 struct PagedPlan {
+  bool chunk;           // there may be sequences for the chunk kernel
   int few;              // a sequence of at most so many rows per key/value head is the decode kernel's (16 or 32), 0: none is
   int decode_parts, chunk_parts;      // most parts of either kernel (1: outputs are written directly)
   int64_t decode_rows;  // rows of one part in the workspace: batch * n_kv_heads * few
   int64_t chunk_rows;   // n_rows * n_q_heads
-  int64_t rows() const { return decode_parts_rows() + chunk_parts_rows(); }
-  int64_t decode_parts_rows() const { return decode_parts > 1 ? decode_parts * decode_rows : 0; }
+  int64_t rows() const { return (decode_parts > 1 ? decode_parts * decode_rows : 0) + chunk_parts_rows(); }
   int64_t chunk_parts_rows() const { return chunk_parts > 1 ? chunk_parts * chunk_rows : 0; }
 };
 constexpr int kDecodeTile = 32;       // keys of a wave's tile
@@ -132,6 +134,7 @@ struct PagedPartial {
   float2* ml;
 };
 
+hipError_t launch_paged_chunk(const PagedAttnArgs& a, const PagedPlan& p, const PagedPartial& ws, hipStream_t s);
 hipError_t launch_paged_decode(const PagedAttnArgs& a, const PagedPlan& p, const PagedPartial& ws, hipStream_t s);
 
 }  // namespace qsvd

@@ -1,66 +1,10 @@
-// Causal attention of new tokens over a paged key/value cache.
-//
-// One wave per (row, query head): 64 keys at a time, a lane each, the online
-// softmax in fp32, then the lanes are the channels of the output.
-#include <math.h>
-
+// Attention over a paged key/value cache: which kernel takes which sequences,
+// how many parts long ones are cut into, and the joining of the parts.
 #include <algorithm>
 
 #include "paged_attn.h"
 
 namespace qsvd {
-
-template <bool BF, int FMT>
-__device__ __forceinline__ float paged_element(const void* pool, int64_t i) {
-  if constexpr (FMT == QSVD_CACHE_F16) return Elem16<BF>::get(pool, i);
-  else if constexpr (FMT == QSVD_CACHE_I8) return (float)reinterpret_cast<const int8_t*>(pool)[i];
-  else return (float)((int)((uint32_t)reinterpret_cast<const uint8_t*>(pool)[i >> 1] << (28 - 4 * (i & 1))) >> 28);
-}
-
-template <bool BF, int DH, int FMT>
-__global__ void __launch_bounds__(64)
-paged_attn_kernel(PagedAttnArgs a, PagedPlan plan) {
-  __shared__ float sq[DH];
-  const int lane = threadIdx.x, h = blockIdx.y;
-  const int64_t m = blockIdx.x;
-  const int b = page_sequence(a.batch.first, a.batch.batch, m, lane, 64);
-  if (b >= a.batch.batch) return;
-  if ((a.batch.first[b + 1] - a.batch.first[b]) * (a.n_q_heads / a.pages.n_kv_heads) <= plan.few) return;
-  const int pos = a.batch.seq_len[b] - (int)(a.batch.first[b + 1] - m);
-  const int hk = h / (a.n_q_heads / a.pages.n_kv_heads);
-  for (int i = lane; i < DH; i += 64) sq[i] = Elem16<BF>::get(a.q, m * a.ldq + h * DH + i);
-  __syncthreads();
-  float mx = -INFINITY, l = 0.f, o[DH / 64] = {};
-  for (int t0 = 0; t0 <= pos; t0 += 64) {
-    const int t = t0 + lane;
-    const int page = t <= pos ? page_of(a.batch, a.pages.n_pages, a.page_bits, b, t) : -1;
-    const int64_t row = (((int64_t)page * a.pages.n_kv_heads + hk) << a.page_bits) + (t & (a.pages.page_size - 1));
-    float x = -INFINITY;
-    if (page >= 0) {
-      float d = 0.f;
-      for (int i = 0; i < DH; ++i) d = fmaf(sq[i], paged_element<BF, FMT>(a.pages.k, row * DH + i), d);
-      if (FMT != QSVD_CACHE_F16) d *= a.pages.k_scale[row];
-      x = d * a.sm_scale;
-    }
-    const float m_new = fmaxf(mx, wave_max(x));
-    const float m_use = m_new == -INFINITY ? 0.f : m_new;
-    const float alpha = expf(mx - m_use), p = expf(x - m_use);
-    mx = m_new;
-    l = l * alpha + wave_sum(p);
-    for (int c = 0; c < DH / 64; ++c) o[c] *= alpha;
-    const float pv = page >= 0 ? (FMT != QSVD_CACHE_F16 ? p * a.pages.v_scale[row] : p) : 0.f;
-    for (int j = 0; j < 64; ++j) {
-      const int pj = __shfl(page, j, 64);
-      const float w = __shfl(pv, j, 64);
-      if (pj < 0) continue;
-      const int64_t rj = (((int64_t)pj * a.pages.n_kv_heads + hk) << a.page_bits) + ((t0 + j) & (a.pages.page_size - 1));
-      for (int c = 0; c < DH / 64; ++c)
-        o[c] = fmaf(w, paged_element<BF, FMT>(a.pages.v, rj * DH + c * 64 + lane), o[c]);
-    }
-  }
-  for (int c = 0; c < DH / 64; ++c)
-    Elem16<BF>::put(a.out, m * a.ldo + h * DH + c * 64 + lane, l == 0.f ? 0.f : o[c] / l);
-}
 
 // The parts of a row joined: a workgroup per row, DH / 4 lanes with four
 // channels each, the parts dealt to its groups of so many lanes.
@@ -113,24 +57,60 @@ paged_join_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
   *reinterpret_cast<uint2*>((uint16_t*)a.out + m * a.ldo + (hk * G + r % G) * DH + 4 * c) = make_uint2(x[0], x[1]);
 }
 
+// The same for the chunk kernel's rows, which are many and of few parts: DH / 4
+// lanes per row.
+template <bool BF, int DH>
+__global__ void __launch_bounds__(256)
+paged_join_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
+  constexpr int LPR = DH / 4;
+  const int c = threadIdx.x % LPR, lane = threadIdx.x & 63;
+  const int64_t row = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
+  const int64_t m = row / a.n_q_heads;
+  const int h = (int)(row - m * a.n_q_heads);
+  const int b = page_sequence(a.batch.first, a.batch.batch, m, lane, LPR);
+  if (m >= a.batch.n_rows || b >= a.batch.batch) return;
+  const int n_new = a.batch.first[b + 1] - a.batch.first[b];
+  if (n_new > a.batch.max_new || n_new * (a.n_q_heads / a.pages.n_kv_heads) <= plan.few) return;
+  float mx = -INFINITY, l = 0.f, y[8] = {};
+  for (int p = 0; p < plan.chunk_parts; ++p) mx = fmaxf(mx, ws.ml[p * plan.chunk_rows + row].x);
+  const float mu = mx == -INFINITY ? 0.f : mx;
+#pragma unroll 4
+  for (int p = 0; p < plan.chunk_parts; ++p) {
+    const float2 ml = ws.ml[p * plan.chunk_rows + row];
+    const f32x4 x = reinterpret_cast<const f32x4*>(ws.o)[(p * plan.chunk_rows + row) * LPR + c];
+    const float e = __builtin_amdgcn_exp2f(ml.x - mu);
+    l += e * ml.y;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) y[k] = fmaf(e, x[k], y[k]);
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) y[k] = l == 0.f ? 0.f : y[k] / l;
+  const i32x4 x = Elem16<BF>::pack(y);
+  *reinterpret_cast<uint2*>((uint16_t*)a.out + m * a.ldo + h * DH + 4 * c) = make_uint2(x[0], x[1]);
+}
+
 template <bool BF, int DH>
 static hipError_t launch_attn(const PagedAttnArgs& a, const PagedPlan& p, const PagedPartial& ws, hipStream_t s) {
-  const int64_t max_rows = (int64_t)a.batch.max_new * (a.n_q_heads / a.pages.n_kv_heads);
   hipError_t e;
-  if (max_rows > p.few) {
-    KernelScope ks("paged_attn", s);
-    auto kern = a.pages.fmt == QSVD_CACHE_I8   ? paged_attn_kernel<BF, DH, QSVD_CACHE_I8>
-                : a.pages.fmt == QSVD_CACHE_I4 ? paged_attn_kernel<BF, DH, QSVD_CACHE_I4>
-                                               : paged_attn_kernel<BF, DH, QSVD_CACHE_F16>;
-    QSVD_LAUNCH(ks, kern, dim3((unsigned)a.batch.n_rows, (unsigned)a.n_q_heads), dim3(64), 0, s, a, p);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+  if (p.chunk) {
+    if ((e = launch_paged_chunk(a, p, ws, s)) != hipSuccess) return e;
+    if (p.chunk_parts > 1) {
+      KernelScope ks("paged_join", s);
+      auto kern = paged_join_chunk_kernel<BF, DH>;
+      constexpr int rows = 256 / (DH / 4);
+      QSVD_LAUNCH(ks, kern, dim3((unsigned)((p.chunk_rows + rows - 1) / rows)), dim3(256), 0, s, a, p, ws);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
   }
   if (p.few > 0) {
-    if ((e = launch_paged_decode(a, p, ws, s)) != hipSuccess) return e;
+    PagedPartial dec = ws;                            // its rows are behind the chunk kernel's
+    dec.o += p.chunk_parts_rows() * DH;
+    dec.ml += p.chunk_parts_rows();
+    if ((e = launch_paged_decode(a, p, dec, s)) != hipSuccess) return e;
     if (p.decode_parts > 1) {
       KernelScope ks("paged_join", s);
       auto kern = paged_join_kernel<BF, DH>;
-      QSVD_LAUNCH(ks, kern, dim3((unsigned)p.decode_rows), dim3(256), 0, s, a, p, ws);
+      QSVD_LAUNCH(ks, kern, dim3((unsigned)p.decode_rows), dim3(256), 0, s, a, p, dec);
       return hipGetLastError();
     }
   }
@@ -140,12 +120,23 @@ static hipError_t launch_attn(const PagedAttnArgs& a, const PagedPlan& p, const 
 static PagedPlan paged_plan(const qsvd_pages& p, const qsvd_page_batch& b, int32_t n_q_heads) {
   PagedPlan o{};
   const int64_t groups = (int64_t)b.batch * p.n_kv_heads, rows = (int64_t)b.max_new * (n_q_heads / p.n_kv_heads);
-  if (rows <= 32) o.few = rows <= 16 ? 16 : 32;
-  else o.few = b.n_rows == (int64_t)b.batch * b.max_new ? 0 : 16;
+  // Sequences of up to 32 rows are the decode kernel's where all are; where some
+  // are longer, those of up to 16 rows, unless all bring the same.
+  if (rows <= 32) {
+    o.few = rows <= 16 ? 16 : 32;
+  } else {
+    o.chunk = true;
+    o.few = b.n_rows == (int64_t)b.batch * b.max_new ? 0 : 16;
+  }
   const int64_t tiles = ((int64_t)b.max_len + kDecodeTile - 1) / kDecodeTile;
   o.decode_parts = (int)std::max<int64_t>(1, std::min({1024 / groups, tiles / kDecodeMinTiles, (int64_t)128}));
-  o.chunk_parts = 1;
   o.decode_rows = groups * o.few;
+  o.chunk_parts = 1;
+  if (o.chunk) {
+    const int64_t seqs = std::min<int64_t>(b.batch, (b.n_rows + b.max_new - 1) / b.max_new);   // about so many are long
+    const int64_t blocks = std::max<int64_t>(1, seqs * p.n_kv_heads * ((rows + 127) / 128));
+    o.chunk_parts = (int)std::max<int64_t>(1, std::min({512 / blocks, tiles / 16, (int64_t)16}));
+  }
   o.chunk_rows = b.n_rows * n_q_heads;
   return o;
 }

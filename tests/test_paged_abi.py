@@ -86,7 +86,7 @@ COMMON = [
     (dict(v_scale=FAKE + 1), UNS), (dict(batch=0), INV), (dict(max_pages=0), INV), (dict(page_table=0), INV),
     (dict(seq_len=0), INV), (dict(first=0), INV), (dict(max_len=-1), INV), (dict(max_new=-1), INV), (dict(n_rows=-1), INV),
     (dict(batch=65537), UNS), (dict(n_rows=1 << 22), UNS), (dict(page_table=FAKE + 2), UNS), (dict(seq_len=FAKE + 1), UNS),
-    (dict(first=FAKE + 2), UNS), (dict(n_rows=0), OK),
+    (dict(first=FAKE + 2), UNS), (dict(max_len=(1 << 30) + 1), UNS), (dict(max_new=1 << 22), UNS), (dict(n_rows=0), OK),
 ]
 
 
@@ -136,6 +136,7 @@ def test_append_refuses_clip(clip):
     (dict(q=0), INV), (dict(out=0), INV), (dict(ldq=248), INV), (dict(ldo=248), INV), (dict(ldq=260), UNS),
     (dict(ldo=260), UNS), (dict(q=FAKE + 8), UNS), (dict(out=FAKE + 8), UNS), (dict(n_q=0), INV), (dict(n_q=3), INV),
     (dict(n_q=258), UNS), (dict(sm=-1.0), INV), (dict(sm=math.inf), INV), (dict(sm=math.nan), INV),
+    (dict(batch=65536, n_kv_heads=8, n_q=8), UNS), (dict(batch=65536, max_new=8192), UNS),
     (dict(n_rows=0, q=0, out=0, ws=0), OK),
 ])
 def test_attention_validation(kw, status):
