@@ -45,10 +45,10 @@ __device__ __forceinline__ RowCode row_code(float amax, float clip, float qm) {
   return r;
 }
 // The low byte (nibble) of the word is the code.  fmed3 and the addition of
-// 1.5 * 2^23 clamp and round half to even (code_bits says how); a NaN element
-// belongs to a row whose `inv` and `up` are 0, and is made 0 first.
+// 1.5 * 2^23 clamp and round half to even (code_bits says how); x has to be a
+// number (a row that has others has `inv` and `up` 0).
 __device__ __forceinline__ uint32_t row_code_bits(float x, const RowCode& r, float qm) {
-  const float t = r.up == 0.f ? 0.f : mul_rn(x, r.up);
+  const float t = mul_rn(x, r.up);
   const float q0 = mul_rn(t, r.inv);
   const float q = fmaf(fmaf(-q0, r.a, t), r.inv, q0);
   return __float_as_uint(add_rn(__builtin_amdgcn_fmed3f(q, -qm, qm), 12582912.0f));

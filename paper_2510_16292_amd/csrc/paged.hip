@@ -41,6 +41,10 @@ __device__ __forceinline__ void store_head(const i32x4& x, void* pool, float* sc
 #pragma unroll
     for (int e = 0; e < 8; ++e) amax = paged_max(amax, fabsf(f[e]));
     const RowCode r = row_code(head_max<DH>(amax), clip, qm);
+    if (__any(r.up == 0.f)) {                       // a vector without codes: its elements may be NaN
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] = r.up == 0.f ? 0.f : f[e];
+    }
     uint32_t b[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) b[e] = row_code_bits(f[e], r, qm);
@@ -79,44 +83,72 @@ __device__ __forceinline__ i32x4 load_head(const void* pool, const float* scales
 
 constexpr int kPagedThreads = 256;
 
+#ifndef PG_H
+#define PG_H 2
+#endif
+constexpr int kPagedHeads = PG_H;
 template <bool BF, int DH, int FMT, bool READ>
 __global__ void __launch_bounds__(kPagedThreads)
 paged_rows_kernel(PagedRowsArgs a) {
   constexpr int LPR = DH / 8;                       // lanes of a head vector
-  const int lane = threadIdx.x & 63, c = threadIdx.x % LPR, h = blockIdx.y;
+  const int lane = threadIdx.x & 63, c = threadIdx.x % LPR, h0 = blockIdx.y * kPagedHeads;
   const int64_t m = (int64_t)blockIdx.x * (kPagedThreads / LPR) + threadIdx.x / LPR;
-  i32x4 kx{}, vx{};
-  uint16_t* kp = (uint16_t*)a.k + m * a.ldk + h * DH + 8 * c;
-  uint16_t* vp = (uint16_t*)a.v + m * a.ldv + h * DH + 8 * c;
+  i32x4 kx[kPagedHeads], vx[kPagedHeads];
+  uint16_t* kp = (uint16_t*)a.k + m * a.ldk + h0 * DH + 8 * c;
+  uint16_t* vp = (uint16_t*)a.v + m * a.ldv + h0 * DH + 8 * c;
   const bool row = m < a.batch.n_rows;
-  if (!READ && row) {
-    kx = *reinterpret_cast<const i32x4*>(kp);
-    vx = *reinterpret_cast<const i32x4*>(vp);
+  if (!READ) {
+#pragma unroll
+    for (int i = 0; i < kPagedHeads; ++i) {
+      kx[i] = vx[i] = i32x4{0, 0, 0, 0};
+      if (row && h0 + i < a.pages.n_kv_heads) {
+        kx[i] = *reinterpret_cast<const i32x4*>(kp + i * DH);
+        vx[i] = *reinterpret_cast<const i32x4*>(vp + i * DH);
+      }
+    }
   }
   const int b = page_sequence(a.batch.first, a.batch.batch, m, lane, LPR);
   const bool live = row && b < a.batch.batch;
-  int64_t at = -1;                                  // the head vector's row in the pool
+  int64_t at = -1;                                  // the row of head h0 in the pool; the next head's is a page further
   if (live) {
     const int pos = a.batch.seq_len[b] - (int)(a.batch.first[b + 1] - m);
     const int page = page_of(a.batch, a.pages.n_pages, a.page_bits, b, pos);
     if (page >= 0)
-      at = (((int64_t)page * a.pages.n_kv_heads + h) << a.page_bits) + (pos & (a.pages.page_size - 1));
+      at = (((int64_t)page * a.pages.n_kv_heads + h0) << a.page_bits) + (pos & (a.pages.page_size - 1));
   }
   if constexpr (READ) {
     if (!live) return;
-    *reinterpret_cast<i32x4*>(kp) = load_head<BF, DH, FMT>(a.pages.k, a.pages.k_scale, at, c);
-    *reinterpret_cast<i32x4*>(vp) = load_head<BF, DH, FMT>(a.pages.v, a.pages.v_scale, at, c);
+#pragma unroll
+    for (int i = 0; i < kPagedHeads; ++i) {
+      kx[i] = vx[i] = i32x4{0, 0, 0, 0};
+      if (h0 + i >= a.pages.n_kv_heads) break;
+      const int64_t r = at < 0 ? -1 : at + ((int64_t)i << a.page_bits);
+      kx[i] = load_head<BF, DH, FMT>(a.pages.k, a.pages.k_scale, r, c);
+      vx[i] = load_head<BF, DH, FMT>(a.pages.v, a.pages.v_scale, r, c);
+    }
+#pragma unroll
+    for (int i = 0; i < kPagedHeads; ++i) {
+      if (h0 + i >= a.pages.n_kv_heads) break;
+      *reinterpret_cast<i32x4*>(kp + i * DH) = kx[i];
+      *reinterpret_cast<i32x4*>(vp + i * DH) = vx[i];
+    }
   } else {
-    if (FMT == QSVD_CACHE_F16 && at < 0) return;    // (codes: every lane takes part in the row's maximum)
-    store_head<BF, DH, FMT>(kx, a.pages.k, a.pages.k_scale, at, c, a.clip);
-    store_head<BF, DH, FMT>(vx, a.pages.v, a.pages.v_scale, at, c, a.clip);
+#pragma unroll
+    for (int i = 0; i < kPagedHeads; ++i) {
+      if (h0 + i >= a.pages.n_kv_heads) break;
+      if (FMT == QSVD_CACHE_F16 && at < 0) break;   // (codes: every lane takes part in the row's maximum)
+      const int64_t r = at < 0 ? -1 : at + ((int64_t)i << a.page_bits);
+      store_head<BF, DH, FMT>(kx[i], a.pages.k, a.pages.k_scale, r, c, a.clip);
+      store_head<BF, DH, FMT>(vx[i], a.pages.v, a.pages.v_scale, r, c, a.clip);
+    }
   }
 }
 
 template <bool BF, int DH, int FMT>
 static hipError_t launch_rows(const PagedRowsArgs& a, bool read, hipStream_t s) {
   constexpr int rows = kPagedThreads / (DH / 8);
-  const dim3 grid((unsigned)((a.batch.n_rows + rows - 1) / rows), (unsigned)a.pages.n_kv_heads);
+  const dim3 grid((unsigned)((a.batch.n_rows + rows - 1) / rows),
+                  (unsigned)((a.pages.n_kv_heads + kPagedHeads - 1) / kPagedHeads));
   KernelScope ks(read ? "paged_read" : "paged_append", s);
   auto kern = read ? paged_rows_kernel<BF, DH, FMT, true> : paged_rows_kernel<BF, DH, FMT, false>;
   QSVD_LAUNCH(ks, kern, grid, dim3(kPagedThreads), 0, s, a);

@@ -11,13 +11,24 @@ typedef __attribute__((address_space(3))) uint8_t lds_byte;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
+// LDS address -> pointer.
+template <class T>
+__device__ __forceinline__ __attribute__((address_space(3))) T* lds_at(uint32_t a) {
+  return (__attribute__((address_space(3))) T*)(uintptr_t)a;
+}
+
 // The products' element type: bf16 over pages of bf16 rows, else fp16 (integer
 // codes are exact in it, and a query is brought into its range by a power of
-// two).
+// two).  The softmax's reference m is the largest score so far to within
+// 2^kSlack: while no score exceeds it by more, nothing is rescaled.  Weights are
+// 2^kShift exp(score - m), so that in fp16 those down to 2^-25 of the largest
+// keep eleven bits; they stay below 2^14, with two bits to spare before one
+// overflows (where scores pass 2^26 their fp32 steps are that coarse).
 template <bool BF>
 struct Mat16 {
   using X8 = f16x8;
   using X4 = f16x4;
+  static constexpr float kShift = 11.f, kSlack = 3.f;
   static __device__ __forceinline__ f32x4 mfma16(X8 a, X8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
   static __device__ __forceinline__ f32x16 mfma32(X8 a, X8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 };
@@ -25,6 +36,7 @@ template <>
 struct Mat16<true> {
   using X8 = bf16x8;
   using X4 = bf16x4;
+  static constexpr float kShift = 0.f, kSlack = 3.f;
   static __device__ __forceinline__ f32x4 mfma16(X8 a, X8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
   static __device__ __forceinline__ f32x16 mfma32(X8 a, X8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 };
@@ -56,7 +68,7 @@ __device__ __forceinline__ f16x8 widen_i4x8_bytes(uint32_t w0, uint32_t w1) {
   widen_i4_bytes(w1, c, d);
   return f16x8{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
 }
-// Eight nibbles of a word as fp16, in the order kNibbleOrder.
+// Eight nibbles of a word as fp16, in the order 0 4 1 5 2 6 3 7.
 __device__ __forceinline__ f16x8 widen_i4x8(uint32_t w) {
   const uint32_t u = w ^ 0x88888888u;
   const f16x2 bias = {(_Float16)1032.f, (_Float16)1032.f};
@@ -77,6 +89,16 @@ __device__ __forceinline__ uint32_t finite16(uint32_t x) {
   const uint32_t lo = (x & ex) == ex ? 0u : x & 0xffffu, hi = (x & ex << 16) == ex << 16 ? 0u : x & 0xffff0000u;
   return lo | hi;
 }
+
+// The unit of value scales: a power of two that is at least the largest so far.
+// (Scales past 2^125 are taken for infinite; changing units changes no bits but
+// those of weights below the normal numbers.)
+constexpr float kLeastUnit = 1.17549435e-38f;         // 2^-126
+__device__ __forceinline__ float sane_scale(float s) { return s <= 4.2535295865117308e37f ? s : 0.f; }
+__device__ __forceinline__ float value_unit(float unit, float top) {
+  return top > unit ? __uint_as_float((__float_as_uint(top) & 0x7f800000u) + 0x00800000u) : unit;
+}
+__device__ __forceinline__ float inverse_unit(float unit) { return __uint_as_float(0x7f000000u - __float_as_uint(unit)); }
 
 // Direct loads into LDS, lane p's bytes to lds + (bytes a lane) p (`lds`
 // wave-uniform): flash.hip says why they are asm.  They complete in order; the
@@ -135,6 +157,7 @@ struct PagedPartial {
 };
 
 hipError_t launch_paged_chunk(const PagedAttnArgs& a, const PagedPlan& p, const PagedPartial& ws, hipStream_t s);
+int paged_decode_resident(const qsvd_pages& p);       // its workgroups that a CU holds
 hipError_t launch_paged_decode(const PagedAttnArgs& a, const PagedPlan& p, const PagedPartial& ws, hipStream_t s);
 
 }  // namespace qsvd

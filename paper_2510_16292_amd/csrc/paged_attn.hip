@@ -16,6 +16,20 @@ paged_join_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
   __shared__ f32x4 s_o[NG][LPR];
   const int c = threadIdx.x % LPR, grp = threadIdx.x / LPR;
   const int pair = blockIdx.x / plan.few, r = blockIdx.x - pair * plan.few;
+  // The first parts are fetched before it is known how many there are.
+  constexpr int kAhead = 4;
+  const int64_t row = (int64_t)pair * plan.few + r, stride = plan.decode_rows;
+  float2 ml[kAhead];
+  f32x4 x[kAhead];
+  auto fetch = [&](int p) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int q = min(p + i * NG, plan.decode_parts - 1);
+      ml[i] = ws.ml[q * stride + row];
+      x[i] = reinterpret_cast<const f32x4*>(ws.o)[(q * stride + row) * LPR + c];
+    }
+  };
+  fetch(grp);
   const int b = pair / a.pages.n_kv_heads, hk = pair - b * a.pages.n_kv_heads, G = a.n_q_heads / a.pages.n_kv_heads;
   const PageSeq sq = page_seq(a.batch, a.page_bits, b);
   if (sq.n_new <= 0 || sq.n_new > plan.few || sq.n_new * G > plan.few || r >= sq.n_new * G) return;
@@ -23,18 +37,20 @@ paged_join_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
   if (parts == 1) return;
   const int64_t m = (int64_t)sq.row0 + r / G;
   if (m < 0 || m >= a.batch.n_rows) return;
-  const int64_t row = (int64_t)pair * plan.few + r, stride = plan.decode_rows;
   float mx = -INFINITY, l = 0.f;
   f32x4 o{};
-  for (int p = grp; p < parts; p += NG) {
-    const float2 ml = ws.ml[p * stride + row];
-    const f32x4 x = reinterpret_cast<const f32x4*>(ws.o)[(p * stride + row) * LPR + c];
-    const float m_new = fmaxf(mx, ml.x), mu = m_new == -INFINITY ? 0.f : m_new;
-    const float ea = __builtin_amdgcn_exp2f(mx - mu), eb = __builtin_amdgcn_exp2f(ml.x - mu);
-    l = l * ea + ml.y * eb;
+  for (int p = grp; p < parts; p += NG * kAhead) {
+    if (p > grp) fetch(p);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] = o[i] * ea + x[i] * eb;
-    mx = m_new;
+    for (int i = 0; i < kAhead; ++i) {
+      if (p + i * NG >= parts) continue;              // (what was fetched there is nothing)
+      const float m_new = fmaxf(mx, ml[i].x), mu = m_new == -INFINITY ? 0.f : m_new;
+      const float ea = __builtin_amdgcn_exp2f(mx - mu), eb = __builtin_amdgcn_exp2f(ml[i].x - mu);
+      l = l * ea + ml[i].y * eb;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) o[k] = o[k] * ea + x[i][k] * eb;
+      mx = m_new;
+    }
   }
   if (c == 0) s_m[grp] = mx, s_l[grp] = l;
   s_o[grp][c] = o;
@@ -53,8 +69,8 @@ paged_join_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
   }
 #pragma unroll
   for (int k = 0; k < 4; ++k) y[k] = l == 0.f ? 0.f : y[k] / l;
-  const i32x4 x = Elem16<BF>::pack(y);
-  *reinterpret_cast<uint2*>((uint16_t*)a.out + m * a.ldo + (hk * G + r % G) * DH + 4 * c) = make_uint2(x[0], x[1]);
+  const i32x4 out = Elem16<BF>::pack(y);
+  *reinterpret_cast<uint2*>((uint16_t*)a.out + m * a.ldo + (hk * G + r % G) * DH + 4 * c) = make_uint2(out[0], out[1]);
 }
 
 // The same for the chunk kernel's rows, which are many and of few parts: DH / 4
@@ -129,7 +145,7 @@ static PagedPlan paged_plan(const qsvd_pages& p, const qsvd_page_batch& b, int32
     o.few = b.n_rows == (int64_t)b.batch * b.max_new ? 0 : 16;
   }
   const int64_t tiles = ((int64_t)b.max_len + kDecodeTile - 1) / kDecodeTile;
-  o.decode_parts = (int)std::max<int64_t>(1, std::min({1024 / groups, tiles / kDecodeMinTiles, (int64_t)128}));
+  o.decode_parts = (int)std::max<int64_t>(1, std::min({256 * paged_decode_resident(p) / groups, tiles / kDecodeMinTiles, (int64_t)128}));
   o.decode_rows = groups * o.few;
   o.chunk_parts = 1;
   if (o.chunk) {

@@ -13,8 +13,8 @@
 //   O^T (dh x 32 rows) += V^T P^T,
 // the second product's operand being the first one's result in its lanes
 // (which keys a lane holds is the same for both), the values read transposed.
-// A key's scale multiplies its scores, a value's its weight, as a fraction of
-// the largest value scale of any tile so far.
+// A key's scale multiplies its scores, a value's its weight, in units of a power
+// of two that bounds the value scales of the tiles so far.
 //
 // Long sequences with few rows are cut into parts along the keys, joined by
 // paged_join_kernel.
@@ -208,9 +208,8 @@ paged_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws, int n_wg, i
       }
     }
   };
-  // Codes of the staged tile into LDS.  Value scales become fractions of vref,
-  // the largest of any tile so far.
-  float vref = 1.17549435e-38f;
+  // Codes of the staged tile into LDS, value scales in units of vref.
+  float vref = kLeastUnit;
   auto widen = [&](int buf) {
     if constexpr (kInt) {
       uint8_t* kb = pc_smem + buf * C::kBuf;
@@ -237,8 +236,8 @@ paged_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws, int n_wg, i
       float* sc = reinterpret_cast<float*>(vb + C::kTile);
       if (w == 0) sc[lane] = scale;
       if (w == 1) {
-        vref = fmaxf(vref, wave_max(scale <= 3.4028234663852886e38f ? scale : 0.f));
-        sc[64 + lane] = scale * __builtin_amdgcn_rcpf(vref);
+        vref = value_unit(vref, wave_max(sane_scale(scale)));
+        sc[64 + lane] = scale * inverse_unit(vref);
         if (lane == 0) sc[128] = vref;
       }
     }
@@ -247,8 +246,22 @@ paged_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws, int n_wg, i
   f32x16 o[OB];
 #pragma unroll
   for (int ob = 0; ob < OB; ++ob) o[ob] = f32x16{};
-  float m_run = -INFINITY, l_run = 0.f, o_unit = 1.17549435e-38f;     // o's unit: the vref it was scaled to
-  typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+  float m_run = -INFINITY, l_run = 0.f, o_unit = kLeastUnit;     // o's unit: the vref it was scaled to
+
+  // LDS addresses of this lane's operands in the present buffer; the next tile's
+  // are `turn` further (everything else about them is a constant offset).
+  uint32_t kaddr[KS], vaddr[OB], saddr = lds0 + 2 * C::kTile + 16 * hl;
+#pragma unroll
+  for (int s = 0; s < KS; ++s) kaddr[s] = lds0 + 16 * pc_kslot<DH>(l32, 2 * s + hl);
+  {
+    const int key = 4 * hl + ((lane & 15) >> 2);
+#pragma unroll
+    for (int ob = 0; ob < OB; ++ob) {
+      const int ch = 32 * ob + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+      vaddr[ob] = lds0 + C::kTile + 16 * pc_vslot<DH>(key, ch >> 3) + 2 * (ch & 7);
+    }
+  }
+  int turn = C::kBuf;
 
   int gone_now = 0;
   if (t0 < t1) {
@@ -314,7 +327,7 @@ paged_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws, int n_wg, i
       auto read_k = [&](int g) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          kf[g & 1][i] = *reinterpret_cast<const X8*>(kb + 16 * pc_kslot<DH>(32 * (i & 1) + l32, 2 * (2 * g + (i >> 1)) + hl));
+          kf[g & 1][i] = *lds_at<X8>(kaddr[2 * g + (i >> 1)] + 32 * (i & 1) * DH * 2);
       };
       read_k(0);
 #pragma unroll
@@ -330,14 +343,10 @@ paged_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws, int n_wg, i
       // group's 16 channels, and receives channel a at keys base .. base + 3.
       X8 vf[2][OB];
       auto read_v = [&](int st) {
-        const int key = 16 * st + 4 * hl + ((lane & 15) >> 2);
 #pragma unroll
         for (int ob = 0; ob < OB; ++ob) {
-          const int ch = 32 * ob + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-              (lds_s16x4*)(vb + 16 * pc_vslot<DH>(key, ch >> 3) + 2 * (ch & 7)));
-          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-              (lds_s16x4*)(vb + 16 * pc_vslot<DH>(key + 8, ch >> 3) + 2 * (ch & 7)));
+          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<s16x4>(vaddr[ob] + 16 * st * DH * 2));
+          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<s16x4>(vaddr[ob] + (16 * st + 8) * DH * 2));
           const X4 a4 = __builtin_bit_cast(X4, lo), b4 = __builtin_bit_cast(X4, hi);
           vf[st & 1][ob] = X8{a4[0], a4[1], a4[2], a4[3], b4[0], b4[1], b4[2], b4[3]};
         }
@@ -347,17 +356,16 @@ paged_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws, int n_wg, i
       // before the branch below: the compiler pads one side of it only.
       asm volatile("s_nop 7\n\ts_nop 7");
       __builtin_amdgcn_sched_barrier(0);
-      const f32x4* sc = reinterpret_cast<const f32x4*>(vb + C::kTile);
       float vfac = 1.f;
       if constexpr (kInt) {
 #pragma unroll
         for (int q4 = 0; q4 < 8; ++q4) {
-          const f32x4 ks = sc[2 * q4 + hl];             // keys 8 q4 + 4 hl ..
+          const f32x4 ks = *lds_at<f32x4>(saddr + 32 * q4);          // keys 8 q4 + 4 hl ..
 #pragma unroll
           for (int i = 0; i < 4; ++i) sacc[q4 >> 2][4 * (q4 & 3) + i] *= ks[i];
         }
-        const float unit = reinterpret_cast<const float*>(sc)[128];
-        vfac = unit == o_unit ? 1.f : o_unit * __builtin_amdgcn_rcpf(unit);
+        const float unit = reinterpret_cast<const float*>(vb + C::kTile)[128];
+        vfac = o_unit * inverse_unit(unit);
         o_unit = unit;
       }
       // tiles wholly before this wave's first query, inside the sequence and without holes need no mask
@@ -376,10 +384,11 @@ paged_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws, int n_wg, i
 #pragma unroll
       for (int v = 1; v < 16; ++v)
         mx = __builtin_elementwise_maximum(mx, __builtin_elementwise_maximum(sacc[0][v], sacc[1][v]));
-      const float m_new = fmaxf(m_run, fa_pair_max(mx) * cs);
-      if (__any(m_new != m_run || vfac != 1.f)) {
-        const float alpha = m_new == m_run ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
-        m_run = m_new;
+      const float m_new = fa_pair_max(mx) * cs;
+      const bool raise = m_new > m_run + M::kSlack;     // (a row's own: others do not change its bits)
+      if (__any(raise) || vfac != 1.f) {
+        const float alpha = raise ? __builtin_amdgcn_exp2f(m_run - m_new) : 1.f;
+        m_run = raise ? m_new : m_run;
         l_run *= alpha;
         const float ao = alpha * vfac;
 #pragma unroll
@@ -392,15 +401,15 @@ paged_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws, int n_wg, i
       for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
-          sacc[kk][v] = __builtin_amdgcn_exp2f(fmaf(sacc[kk][v], cs, -m_use));
+          sacc[kk][v] = __builtin_amdgcn_exp2f(fmaf(sacc[kk][v], cs, M::kShift - m_use));
           ps[v & 3] += sacc[kk][v];
         }
-      l_run += fa_pair_sum((ps[0] + ps[1]) + (ps[2] + ps[3]));
+      l_run += (ps[0] + ps[1]) + (ps[2] + ps[3]);         // (this lane's keys)
       if constexpr (kInt) {
         if (masked) {                                   // (the scale of a value that the query does not see may be NaN)
 #pragma unroll
           for (int q4 = 0; q4 < 8; ++q4) {
-            const f32x4 vs = sc[16 + 2 * q4 + hl];
+            const f32x4 vs = *lds_at<f32x4>(saddr + 256 + 32 * q4);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const int kk = q4 >> 2, v = 4 * (q4 & 3) + i;
@@ -410,7 +419,7 @@ paged_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws, int n_wg, i
         } else {
 #pragma unroll
           for (int q4 = 0; q4 < 8; ++q4) {
-            const f32x4 vs = sc[16 + 2 * q4 + hl];
+            const f32x4 vs = *lds_at<f32x4>(saddr + 256 + 32 * q4);
 #pragma unroll
             for (int i = 0; i < 4; ++i) sacc[q4 >> 2][4 * (q4 & 3) + i] *= vs[i];
           }
@@ -465,7 +474,14 @@ paged_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws, int n_wg, i
       gone_now = gone;
       widen(buf ^ 1);
     }
+#pragma unroll
+    for (int s = 0; s < KS; ++s) kaddr[s] += turn;
+#pragma unroll
+    for (int ob = 0; ob < OB; ++ob) vaddr[ob] += turn;
+    saddr += turn;
+    turn = -turn;
   }
+  l_run = fa_pair_sum(l_run);
   asm volatile("s_nop 7\n\ts_nop 7");
   __builtin_amdgcn_sched_barrier(0);
 
@@ -542,7 +558,7 @@ static hipError_t launch_chunk(const PagedAttnArgs& a, const PagedPlan& p, const
 
 template <bool BF, int DH, int FMT>
 static hipError_t launch_chunk(const PagedAttnArgs& a, const PagedPlan& p, const PagedPartial& ws, hipStream_t s) {
-  return launch_chunk<BF, DH, FMT, 4>(a, p, ws, s);
+  return launch_chunk<BF, DH, FMT, FMT == QSVD_CACHE_F16 ? 4 : 8>(a, p, ws, s);
 }
 
 template <bool BF, int DH>

@@ -15,10 +15,12 @@
 // scores are eight consecutive keys, which is the operand layout of the second
 // product; the values come transposed out of LDS (ds_read_tr).  Codes are
 // widened to fp16, exactly; a key's scale multiplies its scores, a value's its
-// weight (as a fraction of the largest value scale so far, which keeps weights
-// within fp16's normal numbers).
+// weight (in units of a power of two that bounds the value scales so far, which
+// keeps weights within fp16's normal numbers).
 //
 // What bounds it: the bytes of the cache.
+#include <algorithm>
+
 #include "paged_attn.h"
 
 namespace qsvd {
@@ -35,7 +37,7 @@ struct PdCfg {
   static constexpr int kTile = kPdTile * RB;
   static constexpr int kBuf = 2 * kTile + (kInt ? 256 : 0);
   static constexpr int LPT = 2 * NJ + (kInt ? 1 : 0); // direct loads of a tile
-  static constexpr int NB = kTile >= 8192 ? 2 : 3;    // buffers of a wave's ring
+    static constexpr int NB = 2;                        // buffers of a wave's ring
   static constexpr int kJoinRow = DH + 4;             // floats; 16 rows of a wave's outputs, then m, l, vref of each
   static constexpr int kJoin = (16 * kJoinRow + 48) * 4;
   static constexpr int kWave = NB * kBuf > kJoin ? NB * kBuf : kJoin;
@@ -143,10 +145,8 @@ paged_decode_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
   };
 
   // Query rows: column r16 of block n is row 16 n + r16, token row / G.
-  X8 qf[NQ][KS];
-  float cs[NQ];                 // score -> exponent of two
+  i32x4 qx[NQ][KS];
   int qpos[NQ];                 // position, -1: no such row
-  const float log2_scale = a.sm_scale * kFaLog2e;
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
     const int r = 16 * n + r16;
@@ -155,36 +155,45 @@ paged_decode_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
     const bool in = r < n_rows && m >= 0 && m < a.batch.n_rows;
     qpos[n] = in ? sq.len - sq.n_new + tok : -1;
     const uint16_t* qp = (const uint16_t*)a.q + m * a.ldq + head * DH;
-    i32x4 x[KS];
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
       const int e = FMT == QSVD_CACHE_F16 ? 32 * s + 8 * g
                     : FMT == QSVD_CACHE_I8 ? 16 * (4 * (s >> 1) + g) + 8 * (s & 1)
                                            : 8 * KS * g + 8 * s;
-      x[s] = i32x4{0, 0, 0, 0};
-      if (in) x[s] = *reinterpret_cast<const i32x4*>(qp + e);
+      qx[n][s] = i32x4{0, 0, 0, 0};
+      if (in) qx[n][s] = *reinterpret_cast<const i32x4*>(qp + e);
     }
-    cs[n] = log2_scale;
+  }
+  // the first tiles are on their way while the queries arrive
+  if (t0 < t1) {
+    load_pages(t0);
+    issue(t0, 0);
+  }
+  X8 qf[NQ][KS];
+  float cs[NQ];                 // score -> exponent of two
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    cs[n] = a.sm_scale * kFaLog2e;
     if constexpr (kInt && BF) {
       // bf16 queries as fp16: a power of two brings the row's largest to [2^14, 2^15)
       float f[KS][8], amax = 0.f;
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
-        Elem16<true>::unpack(x[s], f[s]);
+        Elem16<true>::unpack(qx[n][s], f[s]);
 #pragma unroll
         for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(f[s][e]));
       }
       amax = fa_rows4_max(amax);
       const int ex = min(max((int)(__float_as_uint(amax) >> 23) - 127, -100), 127);
       const float up = __uint_as_float((uint32_t)(127 + 14 - ex) << 23);
-      cs[n] = log2_scale * __uint_as_float((uint32_t)(127 + ex - 14) << 23);
+      cs[n] *= __uint_as_float((uint32_t)(127 + ex - 14) << 23);
 #pragma unroll
       for (int s = 0; s < KS; ++s)
 #pragma unroll
         for (int e = 0; e < 8; ++e) qf[n][s][e] = (_Float16)(f[s][e] * up);
     } else {
 #pragma unroll
-      for (int s = 0; s < KS; ++s) qf[n][s] = __builtin_bit_cast(X8, x[s]);
+      for (int s = 0; s < KS; ++s) qf[n][s] = __builtin_bit_cast(X8, qx[n][s]);
     }
     if constexpr (FMT == QSVD_CACHE_I4) {
 #pragma unroll
@@ -194,7 +203,7 @@ paged_decode_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
   const int first_pos = sq.len - sq.n_new;              // of the first query: keys up to it need no causal mask
 
   f32x4 o[NQ][OB];
-  float m_run[NQ], l_run[NQ], vref = 1.17549435e-38f;
+  float m_run[NQ], l_run[NQ], vref = kLeastUnit;
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
     m_run[n] = -INFINITY;
@@ -203,21 +212,12 @@ paged_decode_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
     for (int ob = 0; ob < OB; ++ob) o[n][ob] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  if (t0 < t1) {
-    load_pages(t0);
-#pragma unroll
-    for (int i = 0; i < C::NB - 1; ++i)
-      if (t0 + i < t1) issue(t0 + i, i);
-  }
   int buf = 0;
   for (int t = t0; t < t1; ++t) {
-    const int ahead = t + C::NB - 1;
     // (the reads of the buffer that is filled next have returned: their values were used)
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    if (ahead < t1) {
-      issue(ahead, buf + C::NB - 1 >= C::NB ? buf - 1 : buf + C::NB - 1);
-      wait_loads<C::LPT * (C::NB - 1)>();
-    } else if (C::NB > 2 && ahead == t1) {
+    if (t + 1 < t1) {
+      issue(t + 1, buf ^ 1);
       wait_loads<C::LPT>();
     } else {
       wait_loads<0>();
@@ -227,7 +227,7 @@ paged_decode_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
     const uint8_t* kt = pd_smem + w * C::kWave + buf * C::kBuf;
     const uint8_t* vt = kt + C::kTile;
     uint8_t* vt_w = pd_smem + w * C::kWave + buf * C::kBuf + C::kTile;
-    buf = buf + 1 == C::NB ? 0 : buf + 1;
+    buf ^= 1;
     const int k0 = t * kPdTile;
     const int n_here = sq.kend - k0;
     const bool holes = bad0 || bad1 || n_here < kPdTile;
@@ -304,13 +304,13 @@ paged_decode_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
     }
     float rs = 1.f, vfac = 1.f;
     if constexpr (kInt) {
-      float vm = vref;
+      float vm = 0.f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) vm = fmaxf(vm, vs[e] <= 3.4028234663852886e38f ? vs[e] : 0.f);
-      vm = fa_rows4_max(vm);
-      rs = __builtin_amdgcn_rcpf(vm);
-      vfac = vm == vref ? 1.f : vref * rs;
-      vref = vm;
+      for (int e = 0; e < 8; ++e) vm = fmaxf(vm, sane_scale(vs[e]));
+      const float last = vref;
+      vref = value_unit(vref, fa_rows4_max(vm));
+      rs = inverse_unit(vref);
+      vfac = last * rs;
 #pragma unroll
       for (int e = 0; e < 8; ++e) vs[e] *= rs;
     }
@@ -321,10 +321,11 @@ paged_decode_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
 #pragma unroll
       for (int i = 1; i < 4; ++i)
         mx = __builtin_elementwise_maximum(mx, __builtin_elementwise_maximum(sc[n][0][i], sc[n][1][i]));
-      const float m_new = fmaxf(m_run[n], fa_rows4_max(mx) * cs[n]);
-      if (__any(m_new != m_run[n] || vfac != 1.f)) {
-        const float alpha = m_new == m_run[n] ? 1.f : __builtin_amdgcn_exp2f(m_run[n] - m_new);
-        m_run[n] = m_new;
+      const float m_new = fa_rows4_max(mx) * cs[n];
+      const bool raise = m_new > m_run[n] + M::kSlack;  // (a row's own: others do not change its bits)
+      if (__any(raise) || vfac != 1.f) {
+        const float alpha = raise ? __builtin_amdgcn_exp2f(m_run[n] - m_new) : 1.f;
+        m_run[n] = raise ? m_new : m_run[n];
         l_run[n] *= alpha;
         const float ao = alpha * vfac;
 #pragma unroll
@@ -334,7 +335,7 @@ paged_decode_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
       float p[8], sum = 0.f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        p[e] = __builtin_amdgcn_exp2f(fmaf(sc[n][e >> 2][e & 3], cs[n], -m_use));
+        p[e] = __builtin_amdgcn_exp2f(fmaf(sc[n][e >> 2][e & 3], cs[n], M::kShift - m_use));
         sum += p[e];
       }
       l_run[n] += sum;
@@ -527,6 +528,13 @@ paged_decode_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
       }
     }
   }
+}
+
+int paged_decode_resident(const qsvd_pages& p) {
+  const int bytes = p.fmt == QSVD_CACHE_F16  ? (p.head_dim == 128 ? PdCfg<128, QSVD_CACHE_F16>::kLds : PdCfg<64, QSVD_CACHE_F16>::kLds)
+                    : p.fmt == QSVD_CACHE_I8 ? (p.head_dim == 128 ? PdCfg<128, QSVD_CACHE_I8>::kLds : PdCfg<64, QSVD_CACHE_I8>::kLds)
+                                             : (p.head_dim == 128 ? PdCfg<128, QSVD_CACHE_I4>::kLds : PdCfg<64, QSVD_CACHE_I4>::kLds);
+  return std::min(4, 160 * 1024 / bytes);
 }
 
 template <bool BF, int DH, int FMT, int NQ>
