@@ -32,23 +32,29 @@ __device__ __forceinline__ int page_of(const qsvd_page_batch& t, int n_pages, in
 struct RowCode {
   float s, up, inv, a;        // scale; qm 2^-e; 1 / (a 2^-e), 0: codes 0; a 2^-e
 };
+// a / qm rounded once (qm 127 or 7): the product with 1 / qm corrected by its
+// remainder, which is exact.
+__device__ __forceinline__ float over_qm(float a, float qm) {
+  const float y = qm == 127.f ? 1.f / 127.f : 1.f / 7.f, q = mul_rn(a, y);
+  return fmaf(fmaf(-q, qm, a), y, q);
+}
 __device__ __forceinline__ RowCode row_code(float amax, float clip, float qm) {
   RowCode r;
   const float a = mul_rn(clip, amax);
-  r.s = div_rn(a, qm);
-  if (!(a <= 3.4028234663852886e38f)) return RowCode{__uint_as_float(0x7fc00000u), 0.f, 0.f, 1.f};   // infinite or NaN
-  if (a < 1.504632769052528e-36f) return RowCode{1.f, 0.f, 0.f, 1.f};      // 2^-119
+  const bool odd = !(a <= 3.4028234663852886e38f), tiny = a < 1.504632769052528e-36f;      // infinite or NaN; 2^-119
   const int e = (int)(__float_as_uint(a) >> 23) - 127;
+  r.s = odd ? __uint_as_float(0x7fc00000u) : tiny ? 1.f : over_qm(a, qm);
   r.a = __uint_as_float((__float_as_uint(a) & 0x007fffffu) | 0x3f800000u);
-  r.up = ldexpf(qm, -e);
-  r.inv = div_rn(1.f, r.a);
+  const float y = __builtin_amdgcn_rcpf(r.a);
+  r.inv = odd || tiny ? 0.f : fmaf(fmaf(-r.a, y, 1.f), y, y);
+  r.up = odd || tiny ? 0.f : ldexpf(qm, -e);
   return r;
 }
 // The low byte (nibble) of the word is the code.  fmed3 and the addition of
 // 1.5 * 2^23 clamp and round half to even (code_bits says how); x has to be a
 // number (a row that has others has `inv` and `up` 0).
 __device__ __forceinline__ uint32_t row_code_bits(float x, const RowCode& r, float qm) {
-  const float t = mul_rn(x, r.up);
+  const float t = fmaf(x, r.up, 0.f);
   const float q0 = mul_rn(t, r.inv);
   const float q = fmaf(fmaf(-q0, r.a, t), r.inv, q0);
   return __float_as_uint(add_rn(__builtin_amdgcn_fmed3f(q, -qm, qm), 12582912.0f));
