@@ -68,14 +68,20 @@ __device__ __forceinline__ f16x8 widen_i4x8_bytes(uint32_t w0, uint32_t w1) {
   widen_i4_bytes(w1, c, d);
   return f16x8{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
 }
-// Eight nibbles of a word as fp16, in the order 0 4 1 5 2 6 3 7.
-__device__ __forceinline__ f16x8 widen_i4x8(uint32_t w) {
-  const uint32_t u = w ^ 0x88888888u;
+// Eight nibbles of a word as fp16, in the order 0 4 1 5 2 6 3 7 (a nibble with
+// its sign bit turned is 8 more and unsigned; `mask` is 0x000f000f in a register,
+// which lets the mask, the turn and the exponent be one operation).
+__device__ __forceinline__ f16x8 widen_i4x8(uint32_t w, uint32_t mask) {
   const f16x2 bias = {(_Float16)1032.f, (_Float16)1032.f};
   f16x2 p[4];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) p[j] = __builtin_bit_cast(f16x2, ((u >> (4 * j)) & 0x000f000fu) | 0x64006400u) - bias;
+  for (int j = 0; j < 4; ++j) p[j] = __builtin_bit_cast(f16x2, ((w >> (4 * j)) & mask) ^ 0x64086408u) - bias;
   return f16x8{p[0].x, p[0].y, p[1].x, p[1].y, p[2].x, p[2].y, p[3].x, p[3].y};
+}
+__device__ __forceinline__ uint32_t nibble_mask() {
+  uint32_t m = 0x000f000fu;
+  asm volatile("" : "+v"(m));
+  return m;
 }
 template <class X8>
 __device__ __forceinline__ X8 nibble_order(X8 x) {
@@ -94,7 +100,8 @@ __device__ __forceinline__ uint32_t finite16(uint32_t x) {
 // (Scales past 2^125 are taken for infinite; changing units changes no bits but
 // those of weights below the normal numbers.)
 constexpr float kLeastUnit = 1.17549435e-38f;         // 2^-126
-__device__ __forceinline__ float sane_scale(float s) { return s <= 4.2535295865117308e37f ? s : 0.f; }
+constexpr float kMostScale = 4.2535295865117308e37f;  // 2^125
+__device__ __forceinline__ float sane_scale(float s) { return s <= kMostScale ? s : 0.f; }
 __device__ __forceinline__ float value_unit(float unit, float top) {
   return top > unit ? __uint_as_float((__float_as_uint(top) & 0x7f800000u) + 0x00800000u) : unit;
 }
@@ -136,6 +143,7 @@ __device__ __forceinline__ PageSeq page_seq(const qsvd_page_batch& t, int page_b
 struct PagedPlan {
   bool chunk;           // there may be sequences for the chunk kernel
   int few;              // a sequence of at most so many rows per key/value head is the decode kernel's (16 or 32), 0: none is
+  int few_rows;         // most rows of such a sequence
   int decode_parts, chunk_parts;      // most parts of either kernel (1: outputs are written directly)
   int64_t decode_rows;  // rows of one part in the workspace: batch * n_kv_heads * few
   int64_t chunk_rows;   // n_rows * n_q_heads

@@ -15,7 +15,7 @@ paged_join_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
   __shared__ float s_m[NG], s_l[NG];
   __shared__ f32x4 s_o[NG][LPR];
   const int c = threadIdx.x % LPR, grp = threadIdx.x / LPR;
-  const int pair = blockIdx.x / plan.few, r = blockIdx.x - pair * plan.few;
+  const int pair = blockIdx.x / plan.few_rows, r = blockIdx.x - pair * plan.few_rows;
   // The first parts are fetched before it is known how many there are.
   constexpr int kAhead = 4;
   const int64_t row = (int64_t)pair * plan.few + r, stride = plan.decode_rows;
@@ -126,7 +126,8 @@ static hipError_t launch_attn(const PagedAttnArgs& a, const PagedPlan& p, const 
     if (p.decode_parts > 1) {
       KernelScope ks("paged_join", s);
       auto kern = paged_join_kernel<BF, DH>;
-      QSVD_LAUNCH(ks, kern, dim3((unsigned)p.decode_rows), dim3(256), 0, s, a, p, dec);
+      const int64_t blocks = (int64_t)a.batch.batch * a.pages.n_kv_heads * p.few_rows;
+      QSVD_LAUNCH(ks, kern, dim3((unsigned)blocks), dim3(256), 0, s, a, p, dec);
       return hipGetLastError();
     }
   }
@@ -147,6 +148,7 @@ static PagedPlan paged_plan(const qsvd_pages& p, const qsvd_page_batch& b, int32
   const int64_t tiles = ((int64_t)b.max_len + kDecodeTile - 1) / kDecodeTile;
   o.decode_parts = (int)std::max<int64_t>(1, std::min({256 * paged_decode_resident(p) / groups, tiles / kDecodeMinTiles, (int64_t)128}));
   o.decode_rows = groups * o.few;
+  o.few_rows = (int)std::min<int64_t>(o.few, rows);
   o.chunk_parts = 1;
   if (o.chunk) {
     const int64_t seqs = std::min<int64_t>(b.batch, (b.n_rows + b.max_new - 1) / b.max_new);   // about so many are long

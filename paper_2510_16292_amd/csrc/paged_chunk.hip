@@ -210,6 +210,7 @@ paged_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws, int n_wg, i
   };
   // Codes of the staged tile into LDS, value scales in units of vref.
   float vref = kLeastUnit;
+  const uint32_t mask4 = FMT == QSVD_CACHE_I4 ? nibble_mask() : 0u;
   auto widen = [&](int buf) {
     if constexpr (kInt) {
       uint8_t* kb = pc_smem + buf * C::kBuf;
@@ -226,8 +227,8 @@ paged_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws, int n_wg, i
             k8 = widen_i8x8(kx[j][2 * i], kx[j][2 * i + 1]);
             v8 = widen_i8x8(vx[j][2 * i], vx[j][2 * i + 1]);
           } else {
-            k8 = widen_i4x8(kx[j][i]);
-            v8 = widen_i4x8(vx[j][i]);
+            k8 = widen_i4x8(kx[j][i], mask4);
+            v8 = widen_i4x8(vx[j][i], mask4);
           }
           *reinterpret_cast<f16x8*>(kb + 16 * pc_kslot<DH>(row, N * c + i)) = k8;
           *reinterpret_cast<f16x8*>(vb + 16 * pc_vslot<DH>(row, N * c + i)) = v8;

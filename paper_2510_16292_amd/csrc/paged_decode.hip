@@ -212,6 +212,7 @@ paged_decode_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
     for (int ob = 0; ob < OB; ++ob) o[n][ob] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
+  const uint32_t mask4 = FMT == QSVD_CACHE_I4 ? nibble_mask() : 0u;
   int buf = 0;
   for (int t = t0; t < t1; ++t) {
     // (the reads of the buffer that is filled next have returned: their values were used)
@@ -256,11 +257,11 @@ paged_decode_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
       } else if constexpr (DH == 128) {
         const i32x4 x = *reinterpret_cast<const i32x4*>(kr + 16 * (g ^ sw));
 #pragma unroll
-        for (int s = 0; s < KS; ++s) kf[s] = widen_i4x8(x[s]);
+        for (int s = 0; s < KS; ++s) kf[s] = widen_i4x8(x[s], mask4);
       } else {
         const uint2 x = *reinterpret_cast<const uint2*>(kr + 16 * ((g >> 1) ^ sw) + 8 * (g & 1));
-        kf[0] = widen_i4x8(x.x);
-        kf[1] = widen_i4x8(x.y);
+        kf[0] = widen_i4x8(x.x, mask4);
+        kf[1] = widen_i4x8(x.y, mask4);
       }
 #pragma unroll
       for (int s = 0; s < KS; ++s)
@@ -304,9 +305,16 @@ paged_decode_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
     }
     float rs = 1.f, vfac = 1.f;
     if constexpr (kInt) {
-      float vm = 0.f;
+      // (as bits, which order alike; what is not finite is above the rest)
+      uint32_t vb = 0;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) vm = fmaxf(vm, sane_scale(vs[e]));
+      for (int e = 0; e < 8; ++e) vb = max(vb, __float_as_uint(vs[e]));
+      float vm = __uint_as_float(vb);
+      if (__any(!(vm <= kMostScale))) {
+        vm = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) vm = fmaxf(vm, sane_scale(vs[e]));
+      }
       const float last = vref;
       vref = value_unit(vref, fa_rows4_max(vm));
       rs = inverse_unit(vref);
