@@ -151,7 +151,7 @@ static PagedPlan paged_plan(const qsvd_pages& p, const qsvd_page_batch& b, int32
   o.few_rows = (int)std::min<int64_t>(o.few, rows);
   o.chunk_parts = 1;
   if (o.chunk) {
-    const int64_t seqs = std::min<int64_t>(b.batch, (b.n_rows + b.max_new - 1) / b.max_new);   // about so many are long
+    const int64_t seqs = std::max<int64_t>(1, std::min<int64_t>(b.batch, b.n_rows / b.max_new));   // about so many are long
     const int64_t blocks = std::max<int64_t>(1, seqs * p.n_kv_heads * ((rows + 127) / 128));
     o.chunk_parts = (int)std::max<int64_t>(1, std::min({512 / blocks, tiles / 16, (int64_t)16}));
   }

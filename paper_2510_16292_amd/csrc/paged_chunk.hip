@@ -453,19 +453,13 @@ paged_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws, int n_wg, i
             const int row = __builtin_ctzll(left), key = kt0 + row;
             const int64_t at = (((int64_t)page_of(a.batch, a.pages.n_pages, a.page_bits, b, key) * a.pages.n_kv_heads + hk)
                                 << a.page_bits) + (key & (a.pages.page_size - 1));
-            float p = 0.f;
-#pragma unroll
-            for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-              for (int v = 0; v < 16; ++v) p = (row & ~4) == 32 * kk + 8 * (v >> 2) + (v & 3) ? sacc[kk][v] : p;
-            p = __shfl(p, l32 + ((row >> 2) & 1) * 32, 64);
             const bool sees = key <= my_pos;
 #pragma unroll
             for (int ob = 0; ob < OB; ++ob)
 #pragma unroll
               for (int v = 0; v < 16; ++v) {
                 const float x = Elem16<BF>::get(vpool, at * DH + 32 * ob + 8 * (v >> 2) + 4 * hl + (v & 3));
-                if (sees && !(fabsf(x) <= 3.4028234663852886e38f)) o[ob][v] = fmaf(p, x, o[ob][v]);
+                if (sees && !(fabsf(x) <= 3.4028234663852886e38f)) o[ob][v] += x;   // (any weight of it)
               }
           }
         }
@@ -557,9 +551,16 @@ static hipError_t launch_chunk(const PagedAttnArgs& a, const PagedPlan& p, const
   return hipGetLastError();
 }
 
+// Eight waves share the tiles' widening and LDS copies where there are rows for
+// several such workgroups, four (two workgroups per CU) otherwise: us, four and
+// eight waves, heads of 128: 28/4, four chunks of 512 over 8192 tokens int8 368,
+// 319, int4 378, 343, 16-bit 262, 250; one of 1024 over 16384 int8 381, 332; 32
+// heads, 4 x 640 tokens 16-bit 33.2, 41.2, int8 35.7, 45.2; 28/4, 16 x 8 over 4096
+// int8 38.5, 55.1.
 template <bool BF, int DH, int FMT>
 static hipError_t launch_chunk(const PagedAttnArgs& a, const PagedPlan& p, const PagedPartial& ws, hipStream_t s) {
-  return launch_chunk<BF, DH, FMT, FMT == QSVD_CACHE_F16 ? 4 : 8>(a, p, ws, s);
+  const int64_t rows = (int64_t)a.batch.max_new * (a.n_q_heads / a.pages.n_kv_heads);
+  return rows >= 1024 ? launch_chunk<BF, DH, FMT, 8>(a, p, ws, s) : launch_chunk<BF, DH, FMT, 4>(a, p, ws, s);
 }
 
 template <bool BF, int DH>

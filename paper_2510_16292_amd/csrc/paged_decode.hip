@@ -357,10 +357,6 @@ paged_decode_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) p[e] = e < lim ? p[e] : 0.f;
         }
-      } else if (masked) {
-        // keep the scores' place for the weights: rows that are not finite, below
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sc[n][e >> 2][e & 3] = p[e];
       }
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -395,10 +391,6 @@ paged_decode_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
           const uint8_t* vr = vt + row * C::RB;
 #pragma unroll
           for (int n = 0; n < NQ; ++n) {
-            float pr = 0.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) pr = (row & 7) == e ? sc[n][e >> 2][e & 3] : pr;
-            pr = __shfl(pr, ((row >> 3) << 4) + r16, 64);
             const bool sees = k0 + row <= qpos[n];
 #pragma unroll
             for (int ob = 0; ob < OB; ++ob) {
@@ -408,7 +400,7 @@ paged_decode_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
               Elem16<BF>::unpack(i32x4{(int)x.x, (int)x.y, 0, 0}, f);
 #pragma unroll
               for (int i = 0; i < 4; ++i)
-                o[n][ob][i] = sees && !(fabsf(f[i]) <= 3.4028234663852886e38f) ? fmaf(pr, f[i], o[n][ob][i]) : o[n][ob][i];
+                if (sees && !(fabsf(f[i]) <= 3.4028234663852886e38f)) o[n][ob][i] += f[i];   // (any weight of it)
             }
           }
           if (lane < C::CPR) {
