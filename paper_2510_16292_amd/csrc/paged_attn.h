@@ -146,7 +146,7 @@ struct PagedPlan {
   int few_rows;         // most rows of such a sequence
   int decode_parts, chunk_parts;      // most parts of either kernel (1: outputs are written directly)
   int64_t decode_rows;  // rows of one part in the workspace: batch * n_kv_heads * few
-  int64_t chunk_rows;   // n_rows * n_q_heads
+  int64_t chunk_rows;   // n_q_heads rows for each of the step's
   int64_t rows() const { return (decode_parts > 1 ? decode_parts * decode_rows : 0) + chunk_parts_rows(); }
   int64_t chunk_parts_rows() const { return chunk_parts > 1 ? chunk_parts * chunk_rows : 0; }
 };

@@ -84,7 +84,7 @@ paged_join_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
   const int64_t m = row / a.n_q_heads;
   const int h = (int)(row - m * a.n_q_heads);
   const int b = page_sequence(a.batch.first, a.batch.batch, m, lane, LPR);
-  if (m >= a.batch.n_rows || b >= a.batch.batch) return;
+  if (row >= plan.chunk_rows || b >= a.batch.batch) return;
   const int n_new = a.batch.first[b + 1] - a.batch.first[b];
   if (n_new > a.batch.max_new || n_new * (a.n_q_heads / a.pages.n_kv_heads) <= plan.few) return;
   float mx = -INFINITY, l = 0.f, y[8] = {};
@@ -155,7 +155,8 @@ static PagedPlan paged_plan(const qsvd_pages& p, const qsvd_page_batch& b, int32
     const int64_t blocks = std::max<int64_t>(1, seqs * p.n_kv_heads * ((rows + 127) / 128));
     o.chunk_parts = (int)std::max<int64_t>(1, std::min({512 / blocks, tiles / 16, (int64_t)16}));
   }
-  o.chunk_rows = b.n_rows * n_q_heads;
+  // (rows that a sequence has are below batch * max_new; more rows than that are spare)
+  o.chunk_rows = std::min(b.n_rows, (int64_t)b.batch * b.max_new) * n_q_heads;
   return o;
 }
 

@@ -484,8 +484,9 @@ paged_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws, int n_wg, i
   // of every eight channels 0, 4, 1, 5 in the lower half, 2, 6, 3, 7 in the upper).
   const float unit = kInt ? o_unit : 1.f;
   if (plan.chunk_parts > 1) {
-    if (!in || r0 + l32 >= n_rows) return;
-    const int64_t at = (int64_t)part * plan.chunk_rows + m_row * a.n_q_heads + head;
+    const int64_t slot = m_row * a.n_q_heads + head;
+    if (!in || r0 + l32 >= n_rows || slot >= plan.chunk_rows) return;
+    const int64_t at = (int64_t)part * plan.chunk_rows + slot;
     float* dst = ws.o + at * DH;
 #pragma unroll
     for (int ob = 0; ob < OB; ++ob)

@@ -524,6 +524,19 @@ def test_attention_bounds_above_the_lengths():
         p.check(4)
 
 
+def test_attention_spare_rows_and_cut_keys():
+    """Rows behind the step's, with the keys cut into parts: written by neither kernel nor join."""
+    t = H.torch()
+    p = Pool(F16, BF, 1, 128, 64, [2900], [130]).fill()
+    p.rebatch([2900], [130], n_rows=5000)
+    q = t.full((5000, 3 * 128), float("nan"), dtype=t.bfloat16, device="cuda")
+    q[:130] = to16(np.random.default_rng(0).standard_normal((130, 3 * 128)), BF)
+    got = values(p.attend(q, 3))
+    assert (got[130:] == 3.0).all()
+    want, bound = p.want(q[:130], 3)
+    assert_close(got[:130], want, bound)
+
+
 def test_attention_repeats_bit_for_bit():
     for fmt, news in ((F16, [1, 1]), (I8, [200, 1]), (I4, [7, 1])):
         p = Pool(fmt, BF, 2, 128, 32, [2500, 900], news).fill()

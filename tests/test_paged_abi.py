@@ -152,6 +152,18 @@ def test_workspace_size_of_refused_arguments_is_zero():
     assert B.lib().qsvd_paged_attention_workspace_size(None, ctypes.byref(b), 4) == 0
 
 
+def test_workspace_follows_the_rows_there_can_be():
+    """Spare rows behind the step's take no workspace, and one token per sequence no more than its parts."""
+    def size(**kw):
+        p, b = dict(PAGES, n_kv_heads=4, head_dim=128), dict(BATCH, max_len=30000)
+        b.update(kw)
+        return B.qsvd_paged_attention_workspace_size(B.QsvdPages(**p), B.QsvdPageBatch(**b), 28)
+    assert size(batch=1, max_new=100, n_rows=4000000) == size(batch=1, max_new=100, n_rows=101) > 0
+    assert size(batch=1, max_new=100, n_rows=100) <= 16 * 100 * 28 * 520
+    assert size(batch=1, max_new=1, n_rows=1) <= 128 * 4 * 16 * 520
+    assert size(batch=4096, max_new=1, n_rows=4096) == 0
+
+
 # ---------------------------------------------------------------- the oracle
 
 def test_rope_closed_forms():
