@@ -11,6 +11,12 @@ typedef __attribute__((address_space(3))) uint8_t lds_byte;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
+// log2 of a number's mantissa (in [1, 2)); 0 for 0 and what is not finite.
+__device__ __forceinline__ float log2_mantissa(float x) {
+  const bool plain = x > 0.f && x <= 3.4028234663852886e38f;
+  return plain ? __builtin_amdgcn_logf(__uint_as_float((__float_as_uint(x) & 0x007fffffu) | 0x3f800000u)) : 0.f;
+}
+
 // LDS address -> pointer.
 template <class T>
 __device__ __forceinline__ __attribute__((address_space(3))) T* lds_at(uint32_t a) {
@@ -19,16 +25,18 @@ __device__ __forceinline__ __attribute__((address_space(3))) T* lds_at(uint32_t 
 
 // The products' element type: bf16 over pages of bf16 rows, else fp16 (integer
 // codes are exact in it, and a query is brought into its range by a power of
-// two).  The softmax's reference m is the largest score so far to within
-// 2^kSlack: while no score exceeds it by more, nothing is rescaled.  Weights are
-// 2^kShift exp(score - m), so that in fp16 those down to 2^-25 of the largest
-// keep eleven bits; they stay below 2^14, with two bits to spare before one
-// overflows (where scores pass 2^26 their fp32 steps are that coarse).
+// two).  kShift: weights are 2^kShift exp(score - reference), so that in fp16
+// those down to 2^-25 of the largest keep eleven bits; they stay below 2^15, with
+// a bit to spare before one overflows (where scores pass 2^24 their fp32 steps
+// are that coarse).
 template <bool BF>
 struct Mat16 {
   using X8 = f16x8;
   using X4 = f16x4;
-  static constexpr float kShift = 11.f, kSlack = 3.f;
+  static constexpr float kShift = 11.f;
+  static __device__ __forceinline__ float sum2(_Float16 a, _Float16 b, float c) {
+    return __builtin_amdgcn_fdot2(f16x2{a, b}, f16x2{(_Float16)1.f, (_Float16)1.f}, c, false);
+  }
   static __device__ __forceinline__ f32x4 mfma16(X8 a, X8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
   static __device__ __forceinline__ f32x16 mfma32(X8 a, X8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 };
@@ -36,7 +44,11 @@ template <>
 struct Mat16<true> {
   using X8 = bf16x8;
   using X4 = bf16x4;
-  static constexpr float kShift = 0.f, kSlack = 3.f;
+  static constexpr float kShift = 0.f;
+  static __device__ __forceinline__ float sum2(__bf16 a, __bf16 b, float c) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_amdgcn_fdot2_f32_bf16(bf16x2{a, b}, bf16x2{(__bf16)1.f, (__bf16)1.f}, c, false);
+  }
   static __device__ __forceinline__ f32x4 mfma16(X8 a, X8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
   static __device__ __forceinline__ f32x16 mfma32(X8 a, X8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 };

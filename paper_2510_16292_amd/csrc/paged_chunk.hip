@@ -28,6 +28,9 @@
 namespace qsvd {
 
 constexpr int kPcK = 64;        // keys per tile
+// The softmax's reference is the largest score so far to within 2^kChunkSlack:
+// while no score exceeds it by more, nothing is rescaled.
+constexpr float kChunkSlack = 3.f;
 
 template <int DH, int FMT, int NW>
 struct PcCfg {
@@ -38,7 +41,7 @@ struct PcCfg {
   static constexpr int kLoads = kPcK / RPI;                   // such loads of a tile's keys (or values)
   static constexpr int LPW = (kLoads + NW - 1) / NW;          // ... of a wave
   static constexpr int kTile = kPcK * DH * 2;
-  static constexpr int kScales = kInt ? 768 : 0;              // key scales, value weights, their unit
+  static constexpr int kScales = kInt ? 1024 : 0;             // key scales, value weights, their reciprocals, their unit
   static constexpr int kBuf = 2 * kTile + kScales;
   static constexpr int OST = DH + 8;                          // halves of an output row in LDS
   static constexpr int kOut = NW * 32 * OST * 2;
@@ -61,7 +64,7 @@ template <bool BF, int DH, int FMT, int NW>
 __global__ void __launch_bounds__(NW * 64, 2)
 paged_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws, int n_wg, int spread) {
   using C = PcCfg<DH, FMT, NW>;
-  constexpr bool kInt = C::kInt, kBfMat = BF && !kInt;
+  constexpr bool kInt = C::kInt, kBfMat = BF && !kInt, kRoundedSum = kInt && !BF;
   using M = Mat16<kBfMat>;
   using X8 = typename M::X8;
   using X4 = typename M::X4;
@@ -238,8 +241,11 @@ paged_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws, int n_wg, i
       if (w == 0) sc[lane] = scale;
       if (w == 1) {
         vref = value_unit(vref, wave_max(sane_scale(scale)));
-        sc[64 + lane] = scale * inverse_unit(vref);
-        if (lane == 0) sc[128] = vref;
+        const float weight = scale * inverse_unit(vref);
+        sc[64 + lane] = weight;
+        // (a weight of 0 or NaN, of a key that is not there or not seen, adds nothing)
+        if constexpr (kRoundedSum) sc[128 + lane] = weight > 0.f ? __builtin_amdgcn_rcpf(weight) : 0.f;
+        if (lane == 0) sc[192] = vref;
       }
     }
   };
@@ -365,7 +371,7 @@ paged_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws, int n_wg, i
 #pragma unroll
           for (int i = 0; i < 4; ++i) sacc[q4 >> 2][4 * (q4 & 3) + i] *= ks[i];
         }
-        const float unit = reinterpret_cast<const float*>(vb + C::kTile)[128];
+        const float unit = reinterpret_cast<const float*>(vb + C::kTile)[192];
         vfac = o_unit * inverse_unit(unit);
         o_unit = unit;
       }
@@ -386,7 +392,7 @@ paged_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws, int n_wg, i
       for (int v = 1; v < 16; ++v)
         mx = __builtin_elementwise_maximum(mx, __builtin_elementwise_maximum(sacc[0][v], sacc[1][v]));
       const float m_new = fa_pair_max(mx) * cs;
-      const bool raise = m_new > m_run + M::kSlack;     // (a row's own: others do not change its bits)
+      const bool raise = m_new > m_run + kChunkSlack;   // (a row's own: others do not change its bits)
       if (__any(raise) || vfac != 1.f) {
         const float alpha = raise ? __builtin_amdgcn_exp2f(m_run - m_new) : 1.f;
         m_run = raise ? m_new : m_run;
@@ -397,16 +403,18 @@ paged_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws, int n_wg, i
       }
       // (a query with no visible key yet: every exponential below is exp2(-inf) = 0)
       const float m_use = m_run == -INFINITY ? 0.f : m_run;
-      float ps[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          sacc[kk][v] = __builtin_amdgcn_exp2f(fmaf(sacc[kk][v], cs, M::kShift - m_use));
-          ps[v & 3] += sacc[kk][v];
-        }
-      l_run += (ps[0] + ps[1]) + (ps[2] + ps[3]);         // (this lane's keys)
+        for (int v = 0; v < 16; ++v) sacc[kk][v] = __builtin_amdgcn_exp2f(fmaf(sacc[kk][v], cs, M::kShift - m_use));
+      float ps[4] = {0.f, 0.f, 0.f, 0.f};               // (this lane's keys)
       if constexpr (kInt) {
+        if constexpr (!kRoundedSum) {
+#pragma unroll
+          for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) ps[v & 3] += sacc[kk][v];
+        }
         if (masked) {                                   // (the scale of a value that the query does not see may be NaN)
 #pragma unroll
           for (int q4 = 0; q4 < 8; ++q4) {
@@ -438,12 +446,27 @@ paged_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws, int n_wg, i
           if constexpr (kBfMat) pf[e] = (__bf16)p;
           else pf[e] = (_Float16)p;
         }
+        // The weights' sum is taken of the weights as rounded, so that a key that
+        // outweighs the others has exactly its value.  (fp16 outputs; the sum of
+        // exponentials serves bf16 ones as well.)
+        if constexpr (!kInt) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) ps[e] = M::sum2(pf[2 * e], pf[2 * e + 1], ps[e]);
+        } else if constexpr (kRoundedSum) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const f32x4 rs = *lds_at<f32x4>(saddr + 512 + 32 * (2 * st + i));       // 1 / value weight
+#pragma unroll
+            for (int e = 0; e < 4; ++e) ps[e] = fmaf((float)pf[4 * i + e], rs[e], ps[e]);
+          }
+        }
         if (st < 3) read_v(st + 1);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int ob = 0; ob < OB; ++ob) o[ob] = M::mfma32(vf[st & 1][ob], pf, o[ob]);
         __builtin_amdgcn_sched_barrier(0);
       }
+      l_run += (ps[0] + ps[1]) + (ps[2] + ps[3]);
       if constexpr (!kInt) {
         // values that are not finite (0 in the product), for the queries that see them
         if (odd) {

@@ -26,6 +26,14 @@
 namespace qsvd {
 
 constexpr int kPdTile = kDecodeTile, kPdWaves = kDecodeWaves;
+// The softmax's reference is the largest score so far to within 2^kSlack: while
+// no score exceeds it by more, nothing is rescaled.  Where a weight's rounding is
+// as large as the output's own (all but bf16 outputs of fp16 weights) it is the
+// largest itself, so that the weight of its key is a power of two and, where it
+// outweighs the others, not rounded: the error against 64 bits is 1.00 to 1.05
+// times that of the output's rounding alone, 1.3 to 1.4 with a slack of 3.
+template <bool BF, bool INT>
+constexpr float kSlack = BF && INT ? 3.f : 0.f;
 
 template <int DH, int FMT>
 struct PdCfg {
@@ -329,11 +337,20 @@ paged_decode_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
 #pragma unroll
       for (int i = 1; i < 4; ++i)
         mx = __builtin_elementwise_maximum(mx, __builtin_elementwise_maximum(sc[n][0][i], sc[n][1][i]));
-      const float m_new = fa_rows4_max(mx) * cs[n];
-      const bool raise = m_new > m_run[n] + M::kSlack;  // (a row's own: others do not change its bits)
+      mx = fa_rows4_max(mx);
+      const float m_new = mx * cs[n];
+      const bool raise = m_new > m_run[n] + kSlack<BF, kInt>;   // (a row's own: others do not change its bits)
       if (__any(raise) || vfac != 1.f) {
-        const float alpha = raise ? __builtin_amdgcn_exp2f(m_run[n] - m_new) : 1.f;
-        m_run[n] = raise ? m_new : m_run[n];
+        float ref = m_new;
+        if constexpr (kInt && !BF) {
+          // so that the weight of the largest score, its value's scale included, is a power of two
+          float top = 0.f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) top = sc[n][e >> 2][e & 3] == mx ? fmaxf(top, vs[e]) : top;
+          ref += log2_mantissa(fa_rows4_max(top));
+        }
+        const float alpha = raise ? __builtin_amdgcn_exp2f(m_run[n] - ref) : 1.f;
+        m_run[n] = raise ? ref : m_run[n];
         l_run[n] *= alpha;
         const float ao = alpha * vfac;
 #pragma unroll
