@@ -1,5 +1,7 @@
 // What the kernels of the attention over a paged key/value cache share.
 #pragma once
+#include <type_traits>
+
 #include "elem16.h"
 #include "flash.h"
 #include "launch.h"
@@ -156,6 +158,7 @@ struct PagedPlan {
   bool chunk;           // there may be sequences for the chunk kernel
   int few;              // a sequence of at most so many rows per key/value head is the decode kernel's (16 or 32), 0: none is
   int few_rows;         // most rows of such a sequence
+  bool cut;             // chunk_parts is the most, how many follows from all lengths (chunk_cut)
   int decode_parts, chunk_parts;      // most parts of either kernel (1: outputs are written directly)
   int64_t decode_rows;  // rows of one part in the workspace: batch * n_kv_heads * few
   int64_t chunk_rows;   // n_q_heads rows for each of the step's
@@ -168,6 +171,72 @@ constexpr int kDecodeMinTiles = 8;    // ... of a part
 __device__ __forceinline__ int decode_parts(const PagedPlan& p, int kend) {
   const int tiles = (max(kend, 0) + kDecodeTile - 1) / kDecodeTile;
   return max(1, min(p.decode_parts, tiles / kDecodeMinTiles));
+}
+
+// The chunk kernel's parts.  Where there are workgroups for two or more parts of
+// each block of rows, all sequences have as many (PagedPlan::cut false), but none
+// a part of fewer than kChunkMinTiles tiles of 64 keys.  Where there are not, but
+// sequences are long, the parts follow from all lengths, which are on the device:
+// they have at most `tiles` tiles, the least of eight sizes, from what every
+// workgroup that the chip holds would get of the batch's tiles to 1.875 times
+// that, at which the parts are no more than those workgroups (a part more would be
+// a second round), else twice that.  The calling wave's lanes count; all receive it.
+// us, without cutting and with: 28/4 heads of 128, 16 chunks of 100 tokens over
+// 820 to 8192 int4 381, 268, in a batch of 64 with 48 single tokens 390, 305.
+constexpr int kChunkMinTiles = 8;
+constexpr int kChunkMaxBatch = 1024;
+constexpr int kChunkSlots = 512;      // workgroups of 128 rows that the chip holds
+struct ChunkCut {
+  float tiles;
+  int longest;        // tiles of the longest sequence
+};
+__device__ __forceinline__ int chunk_parts(const PagedPlan& p, int tiles, const ChunkCut& c) {
+  const int most = max(1, min(p.chunk_parts, tiles / kChunkMinTiles));
+  return p.cut ? min(most, (int)ceilf((float)tiles / c.tiles)) : most;
+}
+// Sum (or maximum) over the wave by lane moves within rows of sixteen, then
+// between rows; lane 63 has it, and all receive it.
+template <class Op>
+__device__ __forceinline__ float wave_fold(float x, Op op) {
+  auto move = [&](auto ctrl) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), decltype(ctrl)::value, 0xf, 0xf, true));
+  };
+  x = op(x, move(std::integral_constant<int, 0x111>()));     // row_shr 1, 2, 4, 8: lane 15 of a row has the row's
+  x = op(x, move(std::integral_constant<int, 0x112>()));
+  x = op(x, move(std::integral_constant<int, 0x114>()));
+  x = op(x, move(std::integral_constant<int, 0x118>()));
+  float y = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 15));
+#pragma unroll
+  for (int l = 31; l < 64; l += 16) y = op(y, __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), l)));
+  return y;
+}
+__device__ __forceinline__ ChunkCut chunk_cut(const qsvd_page_batch& t, const PagedPlan& p, int page_bits, int n_kv_heads, int G, int lane) {
+  auto add = [](float x, float y) { return x + y; };
+  float blocks = 0.f, sum = 0.f, most = 0.f, parts[8] = {};
+  int tiles = 0;
+  auto look = [&](int b) {                  // this lane's sequence of 64: blocks 0 if it is not the kernel's
+    blocks = 0.f, tiles = 0;
+    if (b >= t.batch) return;
+    const PageSeq s = page_seq(t, page_bits, b);
+    if (s.n_new <= 0 || s.n_new > t.max_new || s.n_new * G <= p.few) return;
+    blocks = (float)((s.n_new * G + 127) / 128), tiles = (max(s.kend, 0) + 63) / 64;
+  };
+  for (int b0 = 0; b0 < t.batch; b0 += 64) {
+    look(b0 + lane);
+    sum += blocks * (float)tiles;
+    most = fmaxf(most, (float)tiles);
+  }
+  const float each = fmaxf(wave_fold(sum, add) * ((float)n_kv_heads / kChunkSlots), 1.f);
+  for (int b0 = 0; b0 < t.batch; b0 += 64) {
+    if (t.batch > 64) look(b0 + lane);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) parts[k] += blocks * (float)chunk_parts(p, tiles, ChunkCut{each * (1.f + 0.125f * k), 0});
+  }
+  ChunkCut c{2.f * each, (int)wave_fold(most, [](float x, float y) { return fmaxf(x, y); })};
+#pragma unroll
+  for (int k = 7; k >= 0; --k)
+    if (wave_fold(parts[k], add) * n_kv_heads <= kChunkSlots) c.tiles = each * (1.f + 0.125f * k);
+  return c;
 }
 
 // Workspace: fp32 rows [rows][head_dim], then (m, l) of each.

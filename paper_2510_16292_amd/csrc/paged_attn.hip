@@ -78,31 +78,37 @@ paged_join_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
 template <bool BF, int DH>
 __global__ void __launch_bounds__(256)
 paged_join_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
-  constexpr int LPR = DH / 4;
-  const int c = threadIdx.x % LPR, lane = threadIdx.x & 63;
-  const int64_t row = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
-  const int64_t m = row / a.n_q_heads;
-  const int h = (int)(row - m * a.n_q_heads);
-  const int b = page_sequence(a.batch.first, a.batch.batch, m, lane, LPR);
-  if (row >= plan.chunk_rows || b >= a.batch.batch) return;
-  const int n_new = a.batch.first[b + 1] - a.batch.first[b];
-  if (n_new > a.batch.max_new || n_new * (a.n_q_heads / a.pages.n_kv_heads) <= plan.few) return;
-  float mx = -INFINITY, l = 0.f, y[8] = {};
-  for (int p = 0; p < plan.chunk_parts; ++p) mx = fmaxf(mx, ws.ml[p * plan.chunk_rows + row].x);
-  const float mu = mx == -INFINITY ? 0.f : mx;
+  constexpr int LPR = DH / 4, kRows = 256 / LPR;
+  const int c = threadIdx.x % LPR, lane = threadIdx.x & 63, G = a.n_q_heads / a.pages.n_kv_heads;
+  ChunkCut cut{};
+  if (plan.cut) cut = chunk_cut(a.batch, plan, a.page_bits, a.pages.n_kv_heads, G, lane);
+  if (plan.cut && chunk_parts(plan, cut.longest, cut) == 1) return;
+  for (int64_t row0 = (int64_t)blockIdx.x * kRows; row0 < plan.chunk_rows; row0 += (int64_t)gridDim.x * kRows) {
+    const int64_t row = row0 + threadIdx.x / LPR, m = row / a.n_q_heads;
+    const int h = (int)(row - m * a.n_q_heads);
+    const int b = page_sequence(a.batch.first, a.batch.batch, m, lane, LPR);
+    if (row >= plan.chunk_rows || b >= a.batch.batch) continue;
+    const PageSeq sq = page_seq(a.batch, a.page_bits, b);
+    if (sq.n_new > a.batch.max_new || sq.n_new * G <= plan.few) continue;
+    const int parts = chunk_parts(plan, (max(sq.kend, 0) + 63) / 64, cut);
+    if (parts == 1) continue;
+    float mx = -INFINITY, l = 0.f, y[8] = {};
+    for (int p = 0; p < parts; ++p) mx = fmaxf(mx, ws.ml[p * plan.chunk_rows + row].x);
+    const float mu = mx == -INFINITY ? 0.f : mx;
 #pragma unroll 4
-  for (int p = 0; p < plan.chunk_parts; ++p) {
-    const float2 ml = ws.ml[p * plan.chunk_rows + row];
-    const f32x4 x = reinterpret_cast<const f32x4*>(ws.o)[(p * plan.chunk_rows + row) * LPR + c];
-    const float e = __builtin_amdgcn_exp2f(ml.x - mu);
-    l += e * ml.y;
+    for (int p = 0; p < parts; ++p) {
+      const float2 ml = ws.ml[p * plan.chunk_rows + row];
+      const f32x4 x = reinterpret_cast<const f32x4*>(ws.o)[(p * plan.chunk_rows + row) * LPR + c];
+      const float e = __builtin_amdgcn_exp2f(ml.x - mu);
+      l += e * ml.y;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) y[k] = fmaf(e, x[k], y[k]);
+      for (int k = 0; k < 4; ++k) y[k] = fmaf(e, x[k], y[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) y[k] = l == 0.f ? 0.f : y[k] / l;
+    const i32x4 x = Elem16<BF>::pack(y);
+    *reinterpret_cast<uint2*>((uint16_t*)a.out + m * a.ldo + h * DH + 4 * c) = make_uint2(x[0], x[1]);
   }
-#pragma unroll
-  for (int k = 0; k < 4; ++k) y[k] = l == 0.f ? 0.f : y[k] / l;
-  const i32x4 x = Elem16<BF>::pack(y);
-  *reinterpret_cast<uint2*>((uint16_t*)a.out + m * a.ldo + h * DH + 4 * c) = make_uint2(x[0], x[1]);
 }
 
 template <bool BF, int DH>
@@ -114,7 +120,8 @@ static hipError_t launch_attn(const PagedAttnArgs& a, const PagedPlan& p, const 
       KernelScope ks("paged_join", s);
       auto kern = paged_join_chunk_kernel<BF, DH>;
       constexpr int rows = 256 / (DH / 4);
-      QSVD_LAUNCH(ks, kern, dim3((unsigned)((p.chunk_rows + rows - 1) / rows)), dim3(256), 0, s, a, p, ws);
+      const int64_t blocks = std::min<int64_t>((p.chunk_rows + rows - 1) / rows, 2048);
+      QSVD_LAUNCH(ks, kern, dim3((unsigned)blocks), dim3(256), 0, s, a, p, ws);
       if ((e = hipGetLastError()) != hipSuccess) return e;
     }
   }
@@ -153,7 +160,15 @@ static PagedPlan paged_plan(const qsvd_pages& p, const qsvd_page_batch& b, int32
   if (o.chunk) {
     const int64_t seqs = std::max<int64_t>(1, std::min<int64_t>(b.batch, b.n_rows / b.max_new));   // about so many are long
     const int64_t blocks = std::max<int64_t>(1, seqs * p.n_kv_heads * ((rows + 127) / 128));
-    o.chunk_parts = (int)std::max<int64_t>(1, std::min({512 / blocks, tiles / 16, (int64_t)16}));
+    const int64_t most = tiles / (2 * kChunkMinTiles);
+    if (b.batch > kChunkMaxBatch) {
+      // (every workgroup would look through all lengths)
+    } else if (2 * blocks <= kChunkSlots) {
+      o.chunk_parts = (int)std::max<int64_t>(1, std::min({kChunkSlots / blocks, most, (int64_t)16}));
+    } else if (blocks < 2 * kChunkSlots && tiles >= 128) {
+      o.cut = true;
+      o.chunk_parts = (int)std::min<int64_t>((2 * kChunkSlots - 1) / blocks + 1, most);
+    }
   }
   // (rows that a sequence has are below batch * max_new; more rows than that are spare)
   o.chunk_rows = std::min(b.n_rows, (int64_t)b.batch * b.max_new) * n_q_heads;

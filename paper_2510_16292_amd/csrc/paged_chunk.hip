@@ -62,7 +62,7 @@ __device__ __forceinline__ int pc_vslot(int row, int c) {
 
 template <bool BF, int DH, int FMT, int NW>
 __global__ void __launch_bounds__(NW * 64, 2)
-paged_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws, int n_wg, int spread) {
+paged_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws, int n_blk, int spread) {
   using C = PcCfg<DH, FMT, NW>;
   constexpr bool kInt = C::kInt, kBfMat = BF && !kInt, kRoundedSum = kInt && !BF;
   using M = Mat16<kBfMat>;
@@ -73,16 +73,67 @@ paged_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws, int n_wg, i
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, hl = lane >> 5;
 
-  const FaWork work = fa_work(blockIdx.x, a.batch.batch * a.pages.n_kv_heads, n_wg, spread);
-  if (!work.any) return;
-  const int grp = work.group, part = work.wg % plan.chunk_parts, blk = work.wg / plan.chunk_parts;
-  const int b = grp / a.pages.n_kv_heads, hk = grp - b * a.pages.n_kv_heads;
   const int G = a.n_q_heads / a.pages.n_kv_heads;
+  ChunkCut cut{};
+  if (plan.cut) cut = chunk_cut(a.batch, plan, a.page_bits, a.pages.n_kv_heads, G, lane);
+  int grp, part, blk;
+  if (spread > 0) {
+    // A head's workgroups on one XCD (flash_map.h), which share its tiles there, the
+    // longest of all heads first; the first parts of all before the second (those
+    // past a sequence's number end at once).
+    const int groups = a.batch.batch * a.pages.n_kv_heads, each = gridDim.x / plan.chunk_parts;
+    part = blockIdx.x / each;
+    const FaWork work = fa_work(blockIdx.x - part * each, groups, n_blk, spread);
+    if (!work.any) return;
+    grp = work.group, blk = work.wg;
+  } else {
+    // Where sequences bring more or less (launch_chunk), the workgroups with work
+    // are counted off sequence by sequence, so that none is launched for the
+    // others and every XCD gets as many.
+    int left = blockIdx.x;
+    grp = -1;
+    for (int b0 = 0; b0 < a.batch.batch && grp < 0; b0 += 64) {
+      int items = 0, n_parts = 1;
+      if (b0 + lane < a.batch.batch) {
+        const PageSeq s = page_seq(a.batch, a.page_bits, b0 + lane);
+        if (s.n_new > 0 && s.n_new <= a.batch.max_new && s.n_new * G > plan.few) {
+          n_parts = chunk_parts(plan, (max(s.kend, 0) + kPcK - 1) / kPcK, cut);
+          items = a.pages.n_kv_heads * ((s.n_new * G + NW * 32 - 1) / (NW * 32)) * n_parts;
+        }
+      }
+      int upto = items;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int x = __shfl_up(upto, o, 64);
+        upto += lane >= o ? x : 0;
+      }
+      const uint64_t mine = __ballot(upto > left);
+      if (mine) {
+        const int l = __builtin_ctzll(mine);
+        left -= __builtin_amdgcn_readlane(upto - items, l);
+        const int heads = a.pages.n_kv_heads, np = __builtin_amdgcn_readlane(n_parts, l);
+        const int blks = __builtin_amdgcn_readlane(items, l) / (heads * np);
+        grp = (b0 + l) * heads + left % heads;
+        part = left / heads % np;
+        blk = blks - 1 - left / (heads * np);
+      } else {
+        left -= __builtin_amdgcn_readlane(upto, 63);
+      }
+    }
+    if (grp < 0) return;
+  }
+  const int b = grp / a.pages.n_kv_heads, hk = grp - b * a.pages.n_kv_heads;
   const PageSeq sq = page_seq(a.batch, a.page_bits, b);
   if (sq.n_new <= 0 || sq.n_new > a.batch.max_new || sq.n_new * G <= plan.few) return;
   const int n_rows = sq.n_new * G;
   const int wg_r0 = blk * NW * 32;
   if (wg_r0 >= n_rows) return;
+  int n_parts = 1;
+  if (plan.chunk_parts > 1) {
+    n_parts = chunk_parts(plan, (max(sq.kend, 0) + kPcK - 1) / kPcK, cut);
+    n_parts = __builtin_amdgcn_readfirstlane(n_parts);
+    if (part >= n_parts) return;
+  }
   const int r0 = wg_r0 + w * 32, my_r = min(r0 + l32, n_rows - 1);
   const bool live = r0 < n_rows;
   const int q_off = sq.len - sq.n_new;                                  // position of the first new token
@@ -92,7 +143,7 @@ paged_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws, int n_wg, i
   const int wg_first = q_off + wg_r0 / G;
   const int wg_end = min(sq.kend, q_off + min(wg_r0 + NW * 32 - 1, n_rows - 1) / G + 1);   // keys the workgroup can see
   const int tiles = wg_end > 0 ? (wg_end + kPcK - 1) / kPcK : 0;
-  const int t0 = (int)((int64_t)tiles * part / plan.chunk_parts), t1 = (int)((int64_t)tiles * (part + 1) / plan.chunk_parts);
+  const int t0 = (int)((int64_t)tiles * part / n_parts), t1 = (int)((int64_t)tiles * (part + 1) / n_parts);
   const int64_t m_row = (int64_t)sq.row0 + tok;
   const bool in = live && m_row >= 0 && m_row < a.batch.n_rows;
 
@@ -506,7 +557,7 @@ paged_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws, int n_wg, i
   // Lane (l32, hl) holds its row at channels 32 ob + 8 vq + 4 hl + i (int4 pages:
   // of every eight channels 0, 4, 1, 5 in the lower half, 2, 6, 3, 7 in the upper).
   const float unit = kInt ? o_unit : 1.f;
-  if (plan.chunk_parts > 1) {
+  if (n_parts > 1) {
     const int64_t slot = m_row * a.n_q_heads + head;
     if (!in || r0 + l32 >= n_rows || slot >= plan.chunk_rows) return;
     const int64_t at = (int64_t)part * plan.chunk_rows + slot;
@@ -566,12 +617,22 @@ static hipError_t launch_chunk(const PagedAttnArgs& a, const PagedPlan& p, const
   const hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   if (e != hipSuccess) return e;
   const int64_t rows = (int64_t)a.batch.max_new * (a.n_q_heads / a.pages.n_kv_heads);
-  const int n_wg = (int)((rows + NW * 32 - 1) / (NW * 32)) * p.chunk_parts;
+  const int n_blk = (int)((rows + NW * 32 - 1) / (NW * 32));
   const int64_t groups = (int64_t)a.batch.batch * a.pages.n_kv_heads;
-  const int spread = fa_parts(groups, n_wg);
-  const int64_t blocks = fa_blocks(groups, n_wg, spread);
+  int spread = fa_parts(groups, n_blk);
+  int64_t blocks = fa_blocks(groups, n_blk, spread) * p.chunk_parts;
+  if ((p.few > 0 || p.cut) && a.batch.batch <= kChunkMaxBatch) {
+    // As many workgroups as there can be work for: whole blocks of the step's rows
+    // and one more per sequence, times their parts; where the parts follow from the
+    // lengths, kChunkSlots more (chunk_cut: at most so many, or half of them and
+    // one for each block).
+    spread = 0;
+    const int64_t n = std::min(a.batch.n_rows, (int64_t)a.batch.batch * a.batch.max_new), G = a.n_q_heads / a.pages.n_kv_heads;
+    blocks = a.pages.n_kv_heads * (n * G / (NW * 32) + std::min<int64_t>(a.batch.batch, n));
+    blocks = p.cut ? blocks + kChunkSlots : blocks * p.chunk_parts;
+  }
   KernelScope ks("paged_chunk", s);
-  QSVD_LAUNCH(ks, kern, dim3((unsigned)blocks), dim3(NW * 64), lds, s, a, p, ws, n_wg, spread);
+  QSVD_LAUNCH(ks, kern, dim3((unsigned)blocks), dim3(NW * 64), lds, s, a, p, ws, n_blk, spread);
   return hipGetLastError();
 }
 

@@ -242,6 +242,39 @@ class Pool:
         return got
 
 
+    def check_large(self, n_q, seed=2):
+        """check() with the oracle's arithmetic in torch's 64 bits on the device, a sequence and head at a time
+        (every page of the sequences has to be there)."""
+        t = H.torch()
+        rng = t.Generator(device="cuda").manual_seed(seed)
+        q = t.randn((self.n_rows, n_q * self.dh), generator=rng, device="cuda").to(dtype_of(self.dt))
+        got = self.attend(q, n_q).double().view(-1, n_q, self.dh)
+        q = q.double().view(-1, n_q, self.dh)
+        stored = [t.from_numpy(np.nan_to_num(x)).cuda() for x, _ in self.stored()]
+        unit = 0.0 if self.fmt == F16 else float(np.nanmax(H.host(self.d.v_scale)))
+        table = t.from_numpy(self.table.astype(np.int64)).cuda()
+        u = HALF_STEP[BF] if self.fmt == F16 and self.dt == BF else HALF_STEP[HALF]
+        group, worst = n_q // self.heads, 0.0
+        for b, (n, new) in enumerate(zip(self.lens, self.news)):
+            if new == 0:
+                continue
+            pages, rows = table[b, :-(-n // self.page)], slice(self.o.first[b], self.o.first[b] + new)
+            hidden = t.ones((new, n), dtype=t.bool, device="cuda").triu(n - new + 1)
+            for h in range(self.heads):
+                k, v = (x[pages, h].reshape(-1, self.dh)[:n] for x in stored)
+                for g in range(h * group, (h + 1) * group):
+                    x = (q[rows, g] @ k.t() * self.dh ** -0.5).masked_fill(hidden, -np.inf)
+                    p = t.softmax(x, 1)
+                    d = (self.dh + 8) * 2.0 ** -24 * (q[rows, g].abs() @ k.abs().t()).max(1, keepdim=True).values * self.dh ** -0.5
+                    want, a = p @ v, p @ v.abs()
+                    top = p.max(1, keepdim=True).values
+                    steps = v.abs().sum(0) if self.fmt == F16 else unit * 127 * n
+                    bound = (u + 2 * d + 2.0 ** -21) * a + 2.0 ** -25 * top * steps
+                    bound = bound + HALF_STEP[self.dt] * (want.abs() + bound) + LEAST[self.dt]
+                    worst = max(worst, float(((got[rows, g] - want).abs() / bound).max()))
+        assert worst <= 1, worst
+
+
 FORMS = [(f, d) for f in (F16, I8, I4) for d in (HALF, BF)]
 FORM_IDS = [f"{FMT[f]}-{'bf16' if d == BF else 'f16'}" for f, d in FORMS]
 
@@ -501,6 +534,15 @@ def test_attention_query_nan_stays_in_its_row(fmt):
 
 
 @pytest.mark.parametrize("new", [1, 100])
+def test_attention_sequences_that_share_pages(new):
+    """Two sequences with the same first pages (a common prompt) read them both."""
+    p = Pool(I8, BF, 2, 128, 16, [100, 90], [new, 1]).fill()
+    p.table[1, :4] = p.table[0, :4]
+    p.rebatch([100, 90], [new, 1])
+    p.check(6)
+
+
+@pytest.mark.parametrize("new", [1, 100])
 def test_attention_strides_and_rows_behind(new):
     t = H.torch()
     p = Pool(I8, HALF, 2, 64, 16, [120, 100], [new, 1]).fill()
@@ -522,6 +564,33 @@ def test_attention_bounds_above_the_lengths():
     for max_len, max_new in ((90, 2), (5000, 2), (5000, 700), (90, 64)):
         p.rebatch([90, 31], [1, 2], max_len=max_len, max_new=max_new)
         p.check(4)
+
+
+@pytest.mark.parametrize("fmt,dt", [(F16, HALF), (I8, BF), (I4, HALF)], ids=["f16-f16", "i8-bf16", "i4-f16"])
+@pytest.mark.parametrize("mixed", [False, True])
+def test_attention_parts_by_all_lengths(fmt, dt, mixed):
+    """Batches that nearly fill the chip, of sequences one of which is much longer
+    than the others: only the longest are cut (and joined)."""
+    lens = [4300, 1500, 900, 130] + [200 + 7 * i for i in range(16)]
+    news = [130] * 20
+    if mixed:
+        lens, news = lens + [5000, 1, 77], news + [1, 1, 2]
+    Pool(fmt, dt, 8, 64, 64, lens, news).fill().check_large(8)
+
+
+@pytest.mark.parametrize("batch", [70, 1100])
+def test_attention_mixed_large_batches(batch):
+    """More sequences than a wave has lanes, and than workgroups look through."""
+    lens = [1 + (37 * b) % 150 for b in range(batch)]
+    news = [min(n, 1 if b % 5 else 50) for b, n in enumerate(lens)]
+    news[3] = news[batch - 2] = 0
+    Pool(I8, HALF, 1, 64, 16, lens, news).fill().check_large(2)
+
+
+@pytest.mark.parametrize("fmt", [F16, I8], ids=["f16", "i8"])
+def test_attention_eight_waves(fmt):
+    """Workgroups of 256 rows: many rows of grouped heads, a last workgroup of few."""
+    Pool(fmt, BF, 2, 128, 64, [700, 300, 260], [161, 300, 150]).fill().check_large(14)
 
 
 def test_attention_spare_rows_and_cut_keys():
