@@ -512,7 +512,11 @@ qsvd_status qsvd_paged_read(const qsvd_pages* pages, const qsvd_page_batch* batc
  * A key or value row that is NaN or infinite reaches only queries that see it.
  * Calls that may overlap need workspaces of their own.  Lengths are read on the
  * device: a captured call may be replayed with other lengths up to max_len and
- * max_new.  A call repeats exactly for the same arguments.
+ * max_new.  A call repeats exactly for the same arguments; how a row's keys are
+ * shared out, and with it the low-order bits of its outputs, follows from batch,
+ * max_len, max_new and n_rows, and where sequences differ in how much they bring
+ * or are long, from the lengths of the others.  A value scale past 2^125 counts
+ * as infinite.
  * Requires n_q_heads a multiple of n_kv_heads and at most 256, batch <= 65536,
  * batch * n_kv_heads <= 2^18, batch * n_kv_heads * ceil(max_new * (n_q_heads /
  * n_kv_heads) / 128) <= 2^22, max_len <= 2^30, n_rows and max_new < 2^22,

@@ -332,6 +332,34 @@ def test_append_and_read(fmt, dt, heads, dh, page, lens, news):
         assert np.array_equal(values(got), want_back)
 
 
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("batch", [65, 129, 300, 2100, 65536])
+def test_append_and_read_large_batches(batch, dh):
+    """Each row to its own sequence: every row of the pool that has a place, and no other, is the row's."""
+    t = H.torch()
+    rng = np.random.default_rng(batch)
+    news = rng.integers(0, 4, batch)
+    news[[0, -1]] = 0, 3
+    news[batch // 2:batch // 2 + 40] = 0
+    lens = news + rng.integers(0, 9, batch)
+    n = int(news.sum())
+    table = rng.permutation(batch).astype(np.int32)[:, None]
+    p = B.DevicePages(F16, HALF, batch, 16, 1, dh)
+    d = B.DevicePageBatch(table, lens.tolist(), news.tolist(), n_rows=n + 5)
+    m = np.arange(n + 5)
+    rows = t.from_numpy(np.tile((m % 2039)[:, None], (1, dh))).half().cuda()
+    rows[:, 1] = t.from_numpy(m // 2039).half().cuda()
+    back = [t.full((n + 5, dh), -1.0, dtype=t.float16, device="cuda") for _ in range(2)]
+    B.check(B.qsvd_paged_append(p.c, d.c, B.ptr(rows), dh, B.ptr(rows), dh, 1.0, B.stream_handle()))
+    B.check(B.qsvd_paged_read(p.c, d.c, B.ptr(back[0]), dh, B.ptr(back[1]), dh, B.stream_handle()))
+    seq = np.repeat(np.arange(batch), news)
+    pos = (lens - np.cumsum(news))[seq] + m[:n]
+    want = t.zeros((batch, 1, 16, dh), dtype=t.float16, device="cuda")
+    want[t.from_numpy(table[seq, 0]).long().cuda(), 0, t.from_numpy(pos).cuda()] = rows[:n]
+    for pool, out in ((p.k, back[0]), (p.v, back[1])):
+        assert t.equal(pool, want) and t.equal(out[:n], rows[:n]) and bool((out[n:] == -1).all())
+
+
 @pytest.mark.parametrize("fmt", [I8, I4], ids=["i8", "i4"])
 @pytest.mark.parametrize("dt", [HALF, BF], ids=["f16", "bf16"])
 @pytest.mark.parametrize("clip", [1.0, 0.7])
