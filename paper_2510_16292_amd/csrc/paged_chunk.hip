@@ -17,9 +17,15 @@
 // of two that bounds the value scales of the tiles so far.
 //
 // Long sequences with few rows are cut into parts along the keys, joined by
-// paged_join_kernel.
+// paged_join_chunk_kernel.
 //
-// What bounds it: the vector operations of the softmax beside the products.
+// What bounds it: the vector operations of the softmax beside the products, which
+// hardly overlap (alone a wave's tile takes 0.47 us of products and 0.5 us of
+// vector operations, together 1.1).  28/4 heads of 128, one prompt of 8192 16-bit
+// tokens: 500 us, 960 TFLOP/s; four chunks of 512 over up to 8192 tokens: 16-bit
+// 247 us, int8 307 us, 720 TFLOP/s (a large product: 1200), the vector units busy
+// 0.46 of the time, the matrix cores 0.28: codes are widened and scales multiplied
+// besides, and 224 workgroups of 256 rows leave 32 CUs without.
 #include <algorithm>
 
 #include "paged_attn.h"
@@ -29,7 +35,9 @@ namespace qsvd {
 
 constexpr int kPcK = 64;        // keys per tile
 // The softmax's reference is the largest score so far to within 2^kChunkSlack:
-// while no score exceeds it by more, nothing is rescaled.
+// while no score exceeds it by more, nothing is rescaled.  (Without slack a wave
+// rescales in three of five tiles: 28/4 heads, four chunks of 512 over 8192 int8
+// tokens 378 us instead of 320.)
 constexpr float kChunkSlack = 3.f;
 
 template <int DH, int FMT, int NW>
