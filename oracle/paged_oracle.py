@@ -77,7 +77,7 @@ class Batch:
                     yield self.first[b] + i, b, n - new + i
 
 
-def attention(q, k, v, batch, n_rows, sm_scale, weight_ulp, v_step=None):
+def attention(q, k, v, batch, n_rows, sm_scale, weight_ulp, v_step=None, sum_ulp=0.0):
     """Outputs [n_rows][Hq][dh] (NaN where no row is) and, beside them, a bound
     of what a kernel may be off before its output's own rounding.
 
@@ -89,7 +89,11 @@ def attention(q, k, v, batch, n_rows, sm_scale, weight_ulp, v_step=None):
       2 d |p_t v_t|            scores off by d = (dh + 8) 2^-24 sum |q k| sm_scale
                                (fp32 sums in any order, the scale and exponent's
                                roundings), in the weights and in their sum,
-      2^-21 |p_t v_t|          the exponentials and fp32 sums of the tiles."""
+      2^-21 |p_t v_t|          the exponentials and fp32 sums of the tiles,
+      sum_ulp |output|         where the weights' sum is of weights rounded by as
+                               much: sum (p_t + e_t) v_t / sum (p_t + e_t) is off by
+                               sum e_t (v_t - output), at most by |e_t v_t| and
+                               |e_t output| together."""
     n_q = q.shape[1]
     heads, dh = k.shape[1], k.shape[3]
     out = np.full((n_rows, n_q, dh), np.nan)
@@ -110,5 +114,5 @@ def attention(q, k, v, batch, n_rows, sm_scale, weight_ulp, v_step=None):
                 out[m, g] = p @ vv / total
                 d = (dh + 8) * 2.0 ** -24 * (np.abs(qq) @ np.abs(kk).T * sm_scale).max(1, keepdims=True)
                 step = np.abs(vv) if v_step is None else v_step[pages, h, rows]
-                bound[m, g] = ((weight_ulp + 2 * d + 2.0 ** -21) * (p @ np.abs(vv)) + 2.0 ** -25 * step.sum(0)) / total
+                bound[m, g] = ((weight_ulp + 2 * d + 2.0 ** -21) * (p @ np.abs(vv)) + 2.0 ** -25 * step.sum(0)) / total + sum_ulp * np.abs(out[m, g])
     return out, bound

@@ -3,7 +3,7 @@
 // A row's head vector is dh elements; dh / 8 lanes hold it, eight elements
 // each, for the key and the value at once.  Per head vector: a = clip max |x|,
 // scale a / Qm, codes rint(x Qm / a) (paged.h); 16-bit pages take the elements
-// as they are.  A workgroup has kPagedRows consecutive rows of one head: their
+// as they are.  A workgroup has consecutive rows of one or two heads: their
 // places in a page follow each other, so that its stores fill whole lines also
 // where a row of codes is half of one.
 //

@@ -217,6 +217,13 @@ class Pool:
                                        out.shape[1], B.ptr(ws), size, B.stream_handle(stream)))
         return out
 
+    def sum_step(self, n_q):
+        """The rounding of the weights that are summed: none for few rows, whose exponentials are summed as they
+        are, nor for bf16 outputs of codes; else that of the weights themselves."""
+        if self.batch.c.max_new * (n_q // self.heads) <= 32 or (self.fmt != F16 and self.dt == BF):
+            return 0.0
+        return HALF_STEP[BF] if self.fmt == F16 and self.dt == BF else HALF_STEP[HALF]
+
     def want(self, q, n_q, sm_scale=None):
         """Oracle output [rows][n_q * dh] (NaN: no row) and bound, its rounding included."""
         (k, _), (v, codes) = self.stored()
@@ -225,7 +232,7 @@ class Pool:
         scale = self.dh ** -0.5 if sm_scale is None else sm_scale
         # weights are rounded to bf16 where the pages hold bf16 rows, else to fp16
         u = HALF_STEP[BF] if self.fmt == F16 and self.dt == BF else HALF_STEP[HALF]
-        out, bound = P.attention(qv, k, v, self.o, qv.shape[0], scale, u, step)
+        out, bound = P.attention(qv, k, v, self.o, qv.shape[0], scale, u, step, self.sum_step(n_q))
         bound = bound + HALF_STEP[self.dt] * (np.abs(out) + bound) + LEAST[self.dt]
         n = qv.shape[0]
         return out.reshape(n, -1), bound.reshape(n, -1)
@@ -269,7 +276,7 @@ class Pool:
                     want, a = p @ v, p @ v.abs()
                     top = p.max(1, keepdim=True).values
                     steps = v.abs().sum(0) if self.fmt == F16 else unit * 127 * n
-                    bound = (u + 2 * d + 2.0 ** -21) * a + 2.0 ** -25 * top * steps
+                    bound = (u + 2 * d + 2.0 ** -21) * a + 2.0 ** -25 * top * steps + self.sum_step(n_q) * want.abs()
                     bound = bound + HALF_STEP[self.dt] * (want.abs() + bound) + LEAST[self.dt]
                     worst = max(worst, float(((got[rows, g] - want).abs() / bound).max()))
         assert worst <= 1, worst
@@ -453,6 +460,27 @@ def test_attention_mixed_batch(fmt, dt):
     lens = [400, 1, 333, 90, 0, 64, 700, 17]
     news = [1, 1, 150, 0, 0, 64, 1, 3]
     Pool(fmt, dt, 2, 128, 32, lens, news).fill().check(8)
+
+
+@pytest.mark.parametrize("seed", range(60))
+def test_attention_drawn(seed):
+    """Formats, heads, pages, lengths and bounds drawn at random, some pages not there."""
+    rng = np.random.default_rng(seed)
+    fmt, dt = FORMS[seed % len(FORMS)]
+    heads, dh, page = int(rng.choice([1, 2, 3, 4, 8])), int(rng.choice([64, 128])), int(rng.choice([16, 32, 64, 1024]))
+    group = min(int(rng.choice([1, 2, 3, 5, 7, 8, 16, 32])), 32 // heads)
+    batch = int(rng.choice([1, 2, 3, 5, 9, 20]))
+    lens = [int(x) for x in rng.integers(0, int(rng.choice([4, 40, 130, 600 if batch < 4 else 200])) + 1, batch)]
+    most = int(rng.choice([1, 6, 100, 1000]))
+    news = [min(n, int(rng.integers(0, most + 1)) if seed % 3 else most) for n in lens]
+    lens, news = lens + [70], news + [1]
+    p = Pool(fmt, dt, heads, dh, page, lens, news, seed=seed).fill(seed)
+    if seed % 4 == 0:
+        gone = rng.random(p.table.shape) < 0.2
+        p.table = np.where(gone, rng.choice([-1, p.n_pages, 2 ** 31 - 1, -2 ** 31], size=p.table.shape), p.table).astype(np.int32)
+    above = [int(x) for x in rng.integers(0, 40, 3)] if seed % 2 else [0, 0, 0]
+    p.rebatch(lens, news, max(lens) + 100 * above[0], max(news) + above[1], sum(news) + above[2])
+    p.check(heads * group, seed=seed, amplitude=float(rng.choice([1, 1, 0.01, 8])))
 
 
 @pytest.mark.parametrize("fmt", [F16, I8, I4], ids=["f16", "i8", "i4"])
