@@ -6,7 +6,7 @@
 // of its four waves works alone on a contiguous share of them, 32 keys at a
 // time, so that nothing in the loop waits for another wave.  A tile's keys,
 // values and scales go straight from memory into a ring of LDS buffers of the
-// wave (direct loads, one or more tiles in flight while one is used).  Per tile,
+// wave (direct loads; int4 codes one tile in flight while one is used).  Per tile,
 // on the 16x16x32 matrix cores, with the query rows (token, head of the group)
 // as columns:
 //   S^T (32 keys x 16 rows) = K Q^T, online softmax per column in fp32,
@@ -21,7 +21,7 @@
 // What bounds it: the bytes of the cache.  32 heads of 128, 16 x 4096 16-bit
 // tokens: 1.07 GB in 187 us, 5.7 TB/s (a streaming read: 5.86); 28/4 heads, 32
 // sequences of up to 8192 int8 tokens: 247 MB in 50 us, 5.0 TB/s.  One sequence of
-// 30001 16-bit tokens of 4 heads, 61 MB, takes 15.7 us, a third of it the first
+// 30001 16-bit tokens of 4 heads, 61 MB, takes 14.6 us, a quarter of it the first
 // loads' latency and the last waves' join.  int4 codes are bound by their widening:
 // 40 heads, 8 sequences of up to 4096 tokens, 159 MB in 38 us, 4.2 TB/s, the vector
 // units busy 0.55 of the time.
@@ -51,10 +51,15 @@ struct PdCfg {
   static constexpr int kTile = kPdTile * RB;
   static constexpr int kBuf = 2 * kTile + (kInt ? 256 : 0);
   static constexpr int LPT = 2 * NJ + (kInt ? 1 : 0); // direct loads of a tile
-  // Buffers of a wave's ring.  Two leave room for two (int8) or four (int4)
-  // workgroups per CU, which hide more latency than a third buffer: 28/4 heads, 32 x
-  // 8192 int8 tokens 53.4 us, with three 66.8.
-  static constexpr int NB = 2;
+  // Buffers of a wave's ring.  One, with the other workgroups of a CU (two of 16-bit
+  // rows of 128, four of int8) hiding its loads, is faster than two with half as
+  // many wherever there are enough: us, two and one, 28/4 heads of 128, 16 bits, 256
+  // sequences of 100 tokens 29.2, 18.5, of 300 48.4, 34.7, of 1000 105, 95.8; int8
+  // 14.6, 11.3; 21.0, 19.0; 53.5, 54.1; 32 heads, 16 x 4096 in 16 bits 193, 191; 4096
+  // sequences of 64 in 16 bits 281, 157; slower in int8 for one or two sequences of one
+  // key/value head, 131072 tokens 21.4, 23.6.  int4 workgroups with two leave room for
+  // four: 256 sequences of 1000 31.2, with one 32.9.
+  static constexpr int NB = FMT == QSVD_CACHE_I4 ? 2 : 1;
   static constexpr int kJoinRow = DH + 4;             // floats; 16 rows of a wave's outputs, then m, l, vref of each
   static constexpr int kJoin = (16 * kJoinRow + 48) * 4;
   static constexpr int kWave = NB * kBuf > kJoin ? NB * kBuf : kJoin;
@@ -82,6 +87,7 @@ template <bool BF, int DH, int FMT, int NQ>
 __global__ void __launch_bounds__(64 * kPdWaves, 2)
 paged_decode_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
   using C = PdCfg<DH, FMT>;
+  constexpr int NB = C::NB;
   constexpr bool kInt = C::kInt, kBfMat = BF && !kInt;
   using M = Mat16<kBfMat>;
   using X8 = typename M::X8;
@@ -234,10 +240,11 @@ paged_decode_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
   for (int t = t0; t < t1; ++t) {
     // (the reads of the buffer that is filled next have returned: their values were used)
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    if (t + 1 < t1) {
+    if (NB > 1 && t + 1 < t1) {
       issue(t + 1, buf ^ 1);
       wait_loads<C::LPT>();
     } else {
+      if (NB == 1 && t > t0) issue(t, 0);
       wait_loads<0>();
     }
     // Which rows are there: all, or (uniform) up to kend and only in pages that are.
@@ -245,7 +252,7 @@ paged_decode_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
     const uint8_t* kt = pd_smem + w * C::kWave + buf * C::kBuf;
     const uint8_t* vt = kt + C::kTile;
     uint8_t* vt_w = pd_smem + w * C::kWave + buf * C::kBuf + C::kTile;
-    buf ^= 1;
+    if (NB > 1) buf ^= 1;
     const int k0 = t * kPdTile;
     const int n_here = sq.kend - k0;
     const bool holes = bad0 || bad1 || n_here < kPdTile;
@@ -556,12 +563,18 @@ paged_decode_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
   }
 }
 
-int paged_decode_resident(const qsvd_pages& p) {
-  const int bytes = p.fmt == QSVD_CACHE_F16  ? (p.head_dim == 128 ? PdCfg<128, QSVD_CACHE_F16>::kLds : PdCfg<64, QSVD_CACHE_F16>::kLds)
-                    : p.fmt == QSVD_CACHE_I8 ? (p.head_dim == 128 ? PdCfg<128, QSVD_CACHE_I8>::kLds : PdCfg<64, QSVD_CACHE_I8>::kLds)
-                                             : (p.head_dim == 128 ? PdCfg<128, QSVD_CACHE_I4>::kLds : PdCfg<64, QSVD_CACHE_I4>::kLds);
-  return std::min(4, 160 * 1024 / bytes);
+// Workgroups that a CU would hold with two buffers a wave: as many as parts are
+// cut for, though with one it holds more.  (More parts cost more in their partial
+// results: one sequence of 30001 16-bit tokens of 4 heads 19.3 us, cut for all that
+// fit 21.5; 16 x 4096 int8 tokens of 32 heads 100, 108.)
+template <int DH>
+static int resident(int fmt) {
+  const int tiles = fmt == QSVD_CACHE_F16  ? PdCfg<DH, QSVD_CACHE_F16>::kBuf
+                    : fmt == QSVD_CACHE_I8 ? PdCfg<DH, QSVD_CACHE_I8>::kBuf
+                                           : PdCfg<DH, QSVD_CACHE_I4>::kBuf;
+  return std::min(4, 160 * 1024 / (kPdWaves * 2 * tiles));
 }
+int paged_decode_resident(const qsvd_pages& p) { return p.head_dim == 128 ? resident<128>(p.fmt) : resident<64>(p.fmt); }
 
 template <bool BF, int DH, int FMT, int NQ>
 static hipError_t launch_decode(const PagedAttnArgs& a, const PagedPlan& p, const PagedPartial& ws, hipStream_t s) {
