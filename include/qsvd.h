@@ -430,7 +430,8 @@ typedef struct {
  * rounded to dtype once.  The angle is formed in revolutions and reduced to
  * [0, 1) in fp64, its sine and cosine taken in fp32 (the hardware's, about
  * 2^-20 absolute).  With the same position on every axis, QSVD_ROPE_RUNNING is
- * the one-axis embedding.  Any int32 position (negative ones turn back).
+ * the one-axis embedding.  Any int32 position; negated ones turn back, which is
+ * also the gradient.
  *   pos     device int32 [n_axes][ldpos]: row m of axis a at pos[a * ldpos + m]
  *   q       device [M][ldq], the n_q_heads heads of a row next to each other
  *   q_out   device [M][ldqo]; may be q itself (same address and stride)

@@ -125,6 +125,17 @@ def test_rope_of_one_position_is_the_one_axis_embedding():
     assert np.array_equal(a, turn(x, p, (32,), 1e4, HALF))
 
 
+@pytest.mark.parametrize("dt", [HALF, BF], ids=["f16", "bf16"])
+def test_rope_at_negated_positions_is_the_gradient(dt):
+    """The transpose: y . turn(x) = turn back(y) . x, each side off by its own bound's dot product."""
+    rng = np.random.default_rng(9)
+    x, y = (P.round16(rng.standard_normal((40, 3, 128)), dt == BF) for _ in range(2))
+    pos = rng.integers(0, 30000, (3, 40))
+    there, back = turn(x, pos, (16, 24, 24), 1e6, dt), turn(y, -pos, (16, 24, 24), 1e6, dt)
+    off = (rope_bound(x, there, dt) * np.abs(y) + rope_bound(y, back, dt) * np.abs(x)).sum(2)
+    assert (np.abs((there * y - back * x).sum(2)) <= 1.01 * off).all()
+
+
 def test_rope_keeps_nan_and_infinity_in_their_pairs():
     x = np.ones((2, 2, 64))
     x[0, 0, 3], x[1, 1, 40] = np.nan, np.inf
