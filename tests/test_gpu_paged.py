@@ -860,6 +860,57 @@ def test_step_captured_and_replayed(fmt, chunk):
     del g
 
 
+@pytest.mark.parametrize("fmt", [F16, I8], ids=["f16", "i8"])
+@pytest.mark.parametrize("spare", [0, 30])
+def test_attention_replayed_with_other_lengths(fmt, spare):
+    """Captured once for a batch of long chunks (parts by all lengths) and replayed with other lengths, other
+    chunks, single tokens and nothing new: each replay is the eager call bit for bit, and right."""
+    t = H.torch()
+    lens, most, hq, dh = [4300, 1500, 900, 130] + [200 + 7 * i for i in range(16)], 130, 8, 64
+    rows = len(lens) * most + spare
+    p = Pool(fmt, HALF, hq, dh, 64, lens, [1] * len(lens)).fill()
+    q = to16(np.random.default_rng(3).standard_normal((rows, hq * dh)), HALF)
+    p.rebatch(lens, [most] * len(lens), 4300, most, rows)
+    c = p.batch
+    size = B.qsvd_paged_attention_workspace_size(p.d.c, c.c, hq)
+    ws = t.full((2, max(size, 1)), 255, dtype=t.uint8, device="cuda")
+    out = t.full((2, rows, hq * dh), 3.0, dtype=t.float16, device="cuda")
+
+    def call(i):
+        B.check(B.qsvd_paged_attention(p.d.c, c.c, B.ptr(q), hq * dh, hq, 0.0, B.ptr(out[i]), hq * dh, B.ptr(ws[i]), size,
+                                       B.stream_handle()))
+
+    call(0)
+    t.cuda.synchronize()
+    g = t.cuda.CUDAGraph()
+    with t.cuda.graph(g):
+        call(1)
+    rng = np.random.default_rng(4)
+    for step in range(5):
+        n = [int(x) for x in (lens if step < 2 else rng.integers(0, np.array(lens) + 1))]
+        new = [min(x, [most, 1, 100, 17, 0][step] if step != 2 or b % 3 else 1) for b, x in enumerate(n)]
+        c.seq_len.copy_(t.tensor(n, dtype=t.int32))
+        c.first.copy_(t.tensor([sum(new[:b]) for b in range(len(n) + 1)], dtype=t.int32))
+        out.fill_(3.0)
+        call(0)
+        g.replay()
+        t.cuda.synchronize()
+        assert t.equal(out[0], out[1]), step
+        assert bool((out[:, sum(new):] == 3).all()) and not bool(t.isnan(out).any())
+        for b in (0, 1, 5):
+            if new[b] == 0:
+                continue
+            m = sum(new[:b + 1]) - 1                      # the last token: sees every key of its sequence
+            (k, _), (v, codes) = p.stored()
+            pages = p.table[b, :-(-n[b] // 64)]
+            kk, vv = (x[pages, 0].reshape(-1, dh)[:n[b]] for x in (k, v))
+            w = np.exp((x := kk @ values(q[m, :dh]) * dh ** -0.5) - x.max())
+            want = w @ vv / w.sum()
+            # (three roundings of 2^-11, of weights, their sum and the output, of at most the largest value)
+            assert np.abs(values(out[0, m, :dh]) - want).max() <= 2.0 ** -9 * np.abs(vv).max(), (step, b)
+    del g
+
+
 def test_two_streams_with_workspaces_of_their_own():
     t = H.torch()
     sides = []
