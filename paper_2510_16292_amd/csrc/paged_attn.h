@@ -159,20 +159,24 @@ struct PagedPlan {
   int few;              // a sequence of at most so many rows per key/value head is the decode kernel's (16 or 32), 0: none is
   int few_rows;         // most rows of such a sequence
   bool cut;             // chunk_parts is the most, how many follows from all lengths (chunk_cut)
+  bool decode_cut;      // the same for decode_parts (decode_cut())
   int decode_parts, chunk_parts;      // most parts of either kernel (1: outputs are written directly)
-  int64_t decode_rows;  // rows of one part in the workspace: batch * n_kv_heads * few
+  int decode_slots;     // workgroups that parts are cut for
+  int64_t decode_rows;  // rows of one part in the workspace: batch * n_kv_heads * few; cut: few for each workgroup
   int64_t chunk_rows;   // n_q_heads rows for each of the step's
-  int64_t rows() const { return (decode_parts > 1 ? decode_parts * decode_rows : 0) + chunk_parts_rows(); }
+  int64_t rows() const { return (decode_parts > 1 ? (decode_cut ? 1 : decode_parts) * decode_rows : 0) + chunk_parts_rows(); }
   int64_t chunk_parts_rows() const { return chunk_parts > 1 ? chunk_parts * chunk_rows : 0; }
 };
 constexpr int kDecodeTile = 32;       // keys of a wave's tile
 constexpr int kDecodeWaves = 4;
 constexpr int kDecodeMinTiles = 8;    // ... of a part
-__device__ __forceinline__ int decode_parts(const PagedPlan& p, int kend) {
-  const int tiles = (max(kend, 0) + kDecodeTile - 1) / kDecodeTile;
-  return max(1, min(p.decode_parts, tiles / kDecodeMinTiles));
-}
-
+// Where the longest sequence's workgroups may have so many tiles, their parts follow
+// from all lengths.  That costs 3 to 10 us and gains where few are long: us, as many
+// parts for each and by all lengths, 28/4 heads of 128, one of 32768 tokens among 63
+// of 1000 in 16 bits 252, 51, in int4 78, 28; 64 of 32768 706, 717; 32 heads, one of
+// 16384 among 15 of 500 int8 177, 48; and with fewer tiles, 28/4 heads, 16
+// sequences of 400 to 8192 in 16 bits (128) 50, 54, 32 heads, 16 of 4096 190, 196.
+constexpr int kDecodeCutTiles = 256;
 // The chunk kernel's parts.  Where there are workgroups for two or more parts of
 // each block of rows, all sequences have as many (PagedPlan::cut false), but none
 // a part of fewer than kChunkMinTiles tiles of 64 keys.  Where there are not, but
@@ -210,33 +214,90 @@ __device__ __forceinline__ float wave_fold(float x, Op op) {
   for (int l = 31; l < 64; l += 16) y = op(y, __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), l)));
   return y;
 }
-__device__ __forceinline__ ChunkCut chunk_cut(const qsvd_page_batch& t, const PagedPlan& p, int page_bits, int n_kv_heads, int G, int lane) {
+// look(b): the blocks (0: not the kernel's) and tiles of sequence b; parts(tiles,
+// cut): its parts.
+template <class Look, class Parts>
+__device__ __forceinline__ ChunkCut cut_by_lengths(int batch, int n_kv_heads, int slots, int lane, Look look, Parts parts_of) {
   auto add = [](float x, float y) { return x + y; };
-  float blocks = 0.f, sum = 0.f, most = 0.f, parts[8] = {};
-  int tiles = 0;
-  auto look = [&](int b) {                  // this lane's sequence of 64: blocks 0 if it is not the kernel's
-    blocks = 0.f, tiles = 0;
-    if (b >= t.batch) return;
-    const PageSeq s = page_seq(t, page_bits, b);
-    if (s.n_new <= 0 || s.n_new > t.max_new || s.n_new * G <= p.few) return;
-    blocks = (float)((s.n_new * G + 127) / 128), tiles = (max(s.kend, 0) + 63) / 64;
-  };
-  for (int b0 = 0; b0 < t.batch; b0 += 64) {
-    look(b0 + lane);
-    sum += blocks * (float)tiles;
-    most = fmaxf(most, (float)tiles);
+  float sum = 0.f, most = 0.f, parts[8] = {};
+  int2 mine = make_int2(0, 0);
+  for (int b0 = 0; b0 < batch; b0 += 64) {
+    mine = b0 + lane < batch ? look(b0 + lane) : make_int2(0, 0);
+    sum += (float)mine.x * (float)mine.y;
+    most = fmaxf(most, (float)mine.y);
   }
-  const float each = fmaxf(wave_fold(sum, add) * ((float)n_kv_heads / kChunkSlots), 1.f);
-  for (int b0 = 0; b0 < t.batch; b0 += 64) {
-    if (t.batch > 64) look(b0 + lane);
+  const float each = fmaxf(wave_fold(sum, add) * ((float)n_kv_heads / slots), 1.f);
+  for (int b0 = 0; b0 < batch; b0 += 64) {
+    if (batch > 64) mine = b0 + lane < batch ? look(b0 + lane) : make_int2(0, 0);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) parts[k] += blocks * (float)chunk_parts(p, tiles, ChunkCut{each * (1.f + 0.125f * k), 0});
+    for (int k = 0; k < 8; ++k) parts[k] += (float)mine.x * (float)parts_of(mine.y, ChunkCut{each * (1.f + 0.125f * k), 0});
   }
   ChunkCut c{2.f * each, (int)wave_fold(most, [](float x, float y) { return fmaxf(x, y); })};
 #pragma unroll
   for (int k = 7; k >= 0; --k)
-    if (wave_fold(parts[k], add) * n_kv_heads <= kChunkSlots) c.tiles = each * (1.f + 0.125f * k);
+    if (wave_fold(parts[k], add) * n_kv_heads <= slots) c.tiles = each * (1.f + 0.125f * k);
   return c;
+}
+__device__ __forceinline__ ChunkCut chunk_cut(const qsvd_page_batch& t, const PagedPlan& p, int page_bits, int n_kv_heads, int G, int lane) {
+  return cut_by_lengths(
+      t.batch, n_kv_heads, kChunkSlots, lane,
+      [&](int b) {
+        const PageSeq s = page_seq(t, page_bits, b);
+        if (s.n_new <= 0 || s.n_new > t.max_new || s.n_new * G <= p.few) return make_int2(0, 0);
+        return make_int2((s.n_new * G + 127) / 128, (max(s.kend, 0) + 63) / 64);
+      },
+      [&](int tiles, const ChunkCut& c) { return chunk_parts(p, tiles, c); });
+}
+
+// The decode kernel's parts: none of fewer than kDecodeMinTiles tiles; as many for
+// every sequence, or, where a workgroup would have long to do, by all lengths, as
+// above.  Then its workgroups are counted off sequence by sequence.
+__device__ __forceinline__ int decode_parts(const PagedPlan& p, int tiles, const ChunkCut& c) {
+  const int most = max(1, min(p.decode_parts, tiles / kDecodeMinTiles));
+  return p.decode_cut ? min(most, (int)ceilf((float)tiles / c.tiles)) : most;
+}
+__device__ __forceinline__ int decode_tiles(int kend) { return (max(kend, 0) + kDecodeTile - 1) / kDecodeTile; }
+struct DecodeWork {
+  int b;              // -1: none
+  int n_parts;
+  int first;          // workgroups before the sequence's, of which part p of head h is p * n_kv_heads + h
+  int longest;        // tiles of the longest sequence
+  ChunkCut cut;
+};
+// The sequence that workgroup `id` is of, or (`of` not negative) sequence `of`.
+__device__ __forceinline__ DecodeWork decode_work(const qsvd_page_batch& t, const PagedPlan& p, int page_bits, int n_kv_heads, int G,
+                                                  int lane, int id, int of) {
+  auto look = [&](int b) {
+    const PageSeq s = page_seq(t, page_bits, b);
+    if (s.n_new <= 0 || s.n_new > p.few || s.n_new * G > p.few) return make_int2(0, 0);
+    return make_int2(1, decode_tiles(s.kend));
+  };
+  const ChunkCut c = cut_by_lengths(t.batch, n_kv_heads, p.decode_slots, lane, look,
+                                    [&](int tiles, const ChunkCut& x) { return decode_parts(p, tiles, x); });
+  DecodeWork w{-1, 1, 0, c.longest, c};
+  for (int b0 = 0; b0 < t.batch && w.b < 0; b0 += 64) {
+    int n = 0;
+    if (b0 + lane < t.batch) {
+      const int2 x = look(b0 + lane);
+      if (x.x) n = decode_parts(p, x.y, c);
+    }
+    int upto = n * n_kv_heads;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int x = __shfl_up(upto, o, 64);
+      upto += lane >= o ? x : 0;
+    }
+    const uint64_t mine = __ballot(of < 0 ? w.first + upto > id : b0 + lane == of);
+    if (mine) {
+      const int l = __builtin_ctzll(mine);
+      w.b = b0 + l;
+      w.n_parts = __builtin_amdgcn_readlane(n, l);
+      w.first += __builtin_amdgcn_readlane(upto, l) - w.n_parts * n_kv_heads;
+    } else {
+      w.first += __builtin_amdgcn_readlane(upto, 63);
+    }
+  }
+  return w;
 }
 
 // Workspace: fp32 rows [rows][head_dim], then (m, l) of each.

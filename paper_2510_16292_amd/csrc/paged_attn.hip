@@ -18,22 +18,29 @@ paged_join_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
   const int pair = blockIdx.x / plan.few_rows, r = blockIdx.x - pair * plan.few_rows;
   // The first parts are fetched before it is known how many there are.
   constexpr int kAhead = 4;
-  const int64_t row = (int64_t)pair * plan.few + r, stride = plan.decode_rows;
+  int64_t row = (int64_t)pair * plan.few + r, stride = plan.decode_rows;
+  int parts = plan.decode_parts;
+  const int b = pair / a.pages.n_kv_heads, hk = pair - b * a.pages.n_kv_heads, G = a.n_q_heads / a.pages.n_kv_heads;
+  if (plan.decode_cut) {
+    const DecodeWork work = decode_work(a.batch, plan, a.page_bits, a.pages.n_kv_heads, G, threadIdx.x & 63, 0, b);
+    parts = work.n_parts;
+    if (parts <= 1) return;
+    row = (int64_t)(work.first + hk) * plan.few + r, stride = (int64_t)a.pages.n_kv_heads * plan.few;
+  }
   float2 ml[kAhead];
   f32x4 x[kAhead];
   auto fetch = [&](int p) {
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
-      const int q = min(p + i * NG, plan.decode_parts - 1);
+      const int q = min(p + i * NG, parts - 1);
       ml[i] = ws.ml[q * stride + row];
       x[i] = reinterpret_cast<const f32x4*>(ws.o)[(q * stride + row) * LPR + c];
     }
   };
   fetch(grp);
-  const int b = pair / a.pages.n_kv_heads, hk = pair - b * a.pages.n_kv_heads, G = a.n_q_heads / a.pages.n_kv_heads;
   const PageSeq sq = page_seq(a.batch, a.page_bits, b);
   if (sq.n_new <= 0 || sq.n_new > plan.few || sq.n_new * G > plan.few || r >= sq.n_new * G) return;
-  const int parts = decode_parts(plan, sq.kend);
+  if (!plan.decode_cut) parts = decode_parts(plan, decode_tiles(sq.kend), ChunkCut{});
   if (parts == 1) return;
   const int64_t m = (int64_t)sq.row0 + r / G;
   if (m < 0 || m >= a.batch.n_rows) return;
@@ -153,8 +160,14 @@ static PagedPlan paged_plan(const qsvd_pages& p, const qsvd_page_batch& b, int32
     o.few = b.n_rows == (int64_t)b.batch * b.max_new ? 0 : 16;
   }
   const int64_t tiles = ((int64_t)b.max_len + kDecodeTile - 1) / kDecodeTile;
-  o.decode_parts = (int)std::max<int64_t>(1, std::min({256 * paged_decode_resident(p) / groups, tiles / kDecodeMinTiles, (int64_t)128}));
+  o.decode_slots = 256 * paged_decode_resident(p);
+  o.decode_parts = (int)std::max<int64_t>(1, std::min({o.decode_slots / groups, tiles / kDecodeMinTiles, (int64_t)128}));
   o.decode_rows = groups * o.few;
+  if (o.few > 0 && b.batch > 1 && b.batch <= kChunkMaxBatch && tiles / o.decode_parts >= kDecodeCutTiles) {
+    o.decode_cut = true;
+    o.decode_parts = (int)std::min<int64_t>(tiles / kDecodeMinTiles, 128);
+    o.decode_rows = (o.decode_slots + groups) * o.few;  // (cut_by_lengths: at most so many workgroups)
+  }
   o.few_rows = (int)std::min<int64_t>(o.few, rows);
   o.chunk_parts = 1;
   if (o.chunk) {

@@ -97,15 +97,24 @@ paged_decode_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r16 = lane & 15, g = lane >> 4;
 
-  const int part = blockIdx.x % plan.decode_parts, grp = blockIdx.x / plan.decode_parts;
-  const int b = grp / a.pages.n_kv_heads, hk = grp - b * a.pages.n_kv_heads;
   const int G = a.n_q_heads / a.pages.n_kv_heads;
+  int part, grp, b, hk, n_parts = 1;
+  if (plan.decode_cut) {
+    const DecodeWork work = decode_work(a.batch, plan, a.page_bits, a.pages.n_kv_heads, G, lane, blockIdx.x, -1);
+    if (work.b < 0) return;
+    const int at = blockIdx.x - work.first;
+    b = work.b, n_parts = work.n_parts, part = at / a.pages.n_kv_heads, hk = at - part * a.pages.n_kv_heads;
+    grp = blockIdx.x;                                   // (its rows in the workspace)
+  } else {
+    part = blockIdx.x % plan.decode_parts, grp = blockIdx.x / plan.decode_parts;
+    b = grp / a.pages.n_kv_heads, hk = grp - b * a.pages.n_kv_heads;
+  }
   const PageSeq sq = page_seq(a.batch, a.page_bits, b);
   const int n_rows = sq.n_new * G;                      // rows of this head
   if (sq.n_new <= 0 || sq.n_new > plan.few || n_rows > plan.few) return;
-  const int n_parts = decode_parts(plan, sq.kend);
+  const int tiles = decode_tiles(sq.kend);
+  if (!plan.decode_cut) n_parts = decode_parts(plan, tiles, ChunkCut{});
   if (part >= n_parts) return;
-  const int tiles = (max(sq.kend, 0) + kPdTile - 1) / kPdTile;
   const int p0 = (int)((int64_t)tiles * part / n_parts), p1 = (int)((int64_t)tiles * (part + 1) / n_parts);
   const int t0 = p0 + (p1 - p0) * w / kPdWaves, t1 = p0 + (p1 - p0) * (w + 1) / kPdWaves;
 
@@ -553,7 +562,7 @@ paged_decode_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
           *reinterpret_cast<uint2*>(op) = make_uint2(x[0], x[1]);
         }
       } else {
-        const int64_t at = (int64_t)part * plan.decode_rows + (int64_t)grp * plan.few + r;
+        const int64_t at = (plan.decode_cut ? 0 : (int64_t)part * plan.decode_rows) + (int64_t)grp * plan.few + r;
 #pragma unroll
         for (int c = 0; c < CT; c += 4)
           *reinterpret_cast<f32x4*>(ws.o + at * DH + ch + c) = f32x4{f[c], f[c + 1], f[c + 2], f[c + 3]};
@@ -582,7 +591,7 @@ static hipError_t launch_decode(const PagedAttnArgs& a, const PagedPlan& p, cons
   constexpr int lds = PdCfg<DH, FMT>::kLds;
   const hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   if (e != hipSuccess) return e;
-  const int64_t blocks = (int64_t)a.batch.batch * a.pages.n_kv_heads * p.decode_parts;
+  const int64_t blocks = p.decode_cut ? p.decode_rows / p.few : (int64_t)a.batch.batch * a.pages.n_kv_heads * p.decode_parts;
   KernelScope ks("paged_decode", s);
   QSVD_LAUNCH(ks, kern, dim3((unsigned)blocks), dim3(64 * kPdWaves), lds, s, a, p, ws);
   return hipGetLastError();

@@ -645,6 +645,21 @@ def test_attention_parts_by_all_lengths(fmt, dt, mixed):
     Pool(fmt, dt, 8, 64, 64, lens, news).fill().check_large(8)
 
 
+@pytest.mark.parametrize("fmt,dt", [(F16, HALF), (I8, BF), (I4, HALF)], ids=["f16-f16", "i8-bf16", "i4-f16"])
+@pytest.mark.parametrize("chunk", [1, 60])
+def test_attention_one_long_among_many(fmt, dt, chunk):
+    """More sequences and heads than the chip holds workgroups of, one of them long: parts by all lengths, where
+    other sequences grow long, and where none is, under the same bounds."""
+    many = [5 + b % 60 for b in range(131)]
+    p = Pool(fmt, dt, 8, 64, 64, many[:40] + [9000] + many[40:], [1] * 132).fill()
+    for lens in (p.lens, many[:40] + [8200] + many[40:], many[:40] + [70] + many[40:], [0] * 132):
+        news = [min(n, 1) for n in lens]
+        news[100] = min(lens[100], chunk)
+        if sum(news):
+            p.rebatch(lens, news, max_len=9000, max_new=chunk, n_rows=132 + chunk)
+            p.check_large(8)
+
+
 @pytest.mark.parametrize("batch", [70, 1100])
 def test_attention_mixed_large_batches(batch):
     """More sequences than a wave has lanes, and than workgroups look through."""
