@@ -177,6 +177,7 @@ constexpr int kDecodeMinTiles = 8;    // ... of a part
 // 16384 among 15 of 500 int8 177, 48; and with fewer tiles, 28/4 heads, 16
 // sequences of 400 to 8192 in 16 bits (128) 50, 54, 32 heads, 16 of 4096 190, 196.
 constexpr int kDecodeCutTiles = 256;
+
 // The chunk kernel's parts.  Where there are workgroups for two or more parts of
 // each block of rows, all sequences have as many (PagedPlan::cut false), but none
 // a part of fewer than kChunkMinTiles tiles of 64 keys.  Where there are not, but
@@ -198,6 +199,7 @@ __device__ __forceinline__ int chunk_parts(const PagedPlan& p, int tiles, const 
   const int most = max(1, min(p.chunk_parts, tiles / kChunkMinTiles));
   return p.cut ? min(most, (int)ceilf((float)tiles / c.tiles)) : most;
 }
+
 // Sum (or maximum) over the wave by lane moves within rows of sixteen, then
 // between rows; lane 63 has it, and all receive it.
 template <class Op>
@@ -214,8 +216,10 @@ __device__ __forceinline__ float wave_fold(float x, Op op) {
   for (int l = 31; l < 64; l += 16) y = op(y, __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), l)));
   return y;
 }
-// look(b): the blocks (0: not the kernel's) and tiles of sequence b; parts(tiles,
-// cut): its parts.
+
+// look(b): the blocks (0: not the kernel's) and tiles of sequence b; parts_of(tiles,
+// cut): its parts.  (Every kernel of a call has to come to the same parts, so no
+// rounding is left to the compiler.)
 template <class Look, class Parts>
 __device__ __forceinline__ ChunkCut cut_by_lengths(int batch, int n_kv_heads, int slots, int lane, Look look, Parts parts_of) {
   auto add = [](float x, float y) { return x + y; };
@@ -223,14 +227,15 @@ __device__ __forceinline__ ChunkCut cut_by_lengths(int batch, int n_kv_heads, in
   int2 mine = make_int2(0, 0);
   for (int b0 = 0; b0 < batch; b0 += 64) {
     mine = b0 + lane < batch ? look(b0 + lane) : make_int2(0, 0);
-    sum += (float)mine.x * (float)mine.y;
+    sum = fmaf((float)mine.x, (float)mine.y, sum);
     most = fmaxf(most, (float)mine.y);
   }
   const float each = fmaxf(wave_fold(sum, add) * ((float)n_kv_heads / slots), 1.f);
   for (int b0 = 0; b0 < batch; b0 += 64) {
     if (batch > 64) mine = b0 + lane < batch ? look(b0 + lane) : make_int2(0, 0);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) parts[k] += (float)mine.x * (float)parts_of(mine.y, ChunkCut{each * (1.f + 0.125f * k), 0});
+    for (int k = 0; k < 8; ++k)
+      parts[k] = fmaf((float)mine.x, (float)parts_of(mine.y, ChunkCut{each * (1.f + 0.125f * k), 0}), parts[k]);
   }
   ChunkCut c{2.f * each, (int)wave_fold(most, [](float x, float y) { return fmaxf(x, y); })};
 #pragma unroll
@@ -261,8 +266,6 @@ struct DecodeWork {
   int b;              // -1: none
   int n_parts;
   int first;          // workgroups before the sequence's, of which part p of head h is p * n_kv_heads + h
-  int longest;        // tiles of the longest sequence
-  ChunkCut cut;
 };
 // The sequence that workgroup `id` is of, or (`of` not negative) sequence `of`.
 __device__ __forceinline__ DecodeWork decode_work(const qsvd_page_batch& t, const PagedPlan& p, int page_bits, int n_kv_heads, int G,
@@ -274,7 +277,7 @@ __device__ __forceinline__ DecodeWork decode_work(const qsvd_page_batch& t, cons
   };
   const ChunkCut c = cut_by_lengths(t.batch, n_kv_heads, p.decode_slots, lane, look,
                                     [&](int tiles, const ChunkCut& x) { return decode_parts(p, tiles, x); });
-  DecodeWork w{-1, 1, 0, c.longest, c};
+  DecodeWork w{-1, 1, 0};
   for (int b0 = 0; b0 < t.batch && w.b < 0; b0 += 64) {
     int n = 0;
     if (b0 + lane < t.batch) {
