@@ -77,15 +77,19 @@ class Batch:
                     yield self.first[b] + i, b, n - new + i
 
 
-def attention(q, k, v, batch, n_rows, sm_scale, weight_ulp, v_step=None, sum_ulp=0.0):
+def attention(q, k, v, batch, n_rows, sm_scale, weight_ulp, v_step=None, sum_ulp=0.0, shift=11):
     """Outputs [n_rows][Hq][dh] (NaN where no row is) and, beside them, a bound
     of what a kernel may be off before its output's own rounding.
 
     k, v: stored values [pages][heads][page][dh] in float64.  The bound counts,
     for weights p_t relative to the largest:
       weight_ulp |p_t v_t|     each weight rounded to 16 bits,
-      2^-25 step_t             or, below the normal fp16 numbers, by that much of
-                               the value's unit (step_t, |v_t| or v_step |code|),
+      2^-25-shift |v_t|        or, below the normal fp16 numbers, by 2^-25, where the
+                               largest weight is 2^shift (16-bit rows),
+      2^-23-shift step_t       the same over codes, whose weights take their value's
+                               scale: in units of a power of two of at most twice the
+                               largest scale (step_t is that scale times |code|), the
+                               largest weight at least 2^(shift - 1),
       2 d |p_t v_t|            scores off by d = (dh + 8) 2^-24 sum |q k| sm_scale
                                (fp32 sums in any order, the scale and exponent's
                                roundings), in the weights and in their sum,
@@ -113,6 +117,6 @@ def attention(q, k, v, batch, n_rows, sm_scale, weight_ulp, v_step=None, sum_ulp
                 total = p.sum(1, keepdims=True)
                 out[m, g] = p @ vv / total
                 d = (dh + 8) * 2.0 ** -24 * (np.abs(qq) @ np.abs(kk).T * sm_scale).max(1, keepdims=True)
-                step = np.abs(vv) if v_step is None else v_step[pages, h, rows]
-                bound[m, g] = ((weight_ulp + 2 * d + 2.0 ** -21) * (p @ np.abs(vv)) + 2.0 ** -25 * step.sum(0)) / total + sum_ulp * np.abs(out[m, g])
+                step = 2.0 ** -25 * np.abs(vv) if v_step is None else 2.0 ** -23 * v_step[pages, h, rows]
+                bound[m, g] = ((weight_ulp + 2 * d + 2.0 ** -21) * (p @ np.abs(vv)) + 2.0 ** -shift * step.sum(0)) / total + sum_ulp * np.abs(out[m, g])
     return out, bound
