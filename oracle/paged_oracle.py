@@ -77,7 +77,8 @@ class Batch:
                     yield self.first[b] + i, b, n - new + i
 
 
-def attention(q, k, v, batch, n_rows, sm_scale, weight_ulp, v_step=None, sum_ulp=0.0, shift=11):
+def attention(q, k, v, batch, n_rows, sm_scale, weight_ulp, v_step=None, sum_ulp=0.0, shift=11,
+              sum_least=2.0 ** -28):
     """Outputs [n_rows][Hq][dh] (NaN where no row is) and, beside them, a bound
     of what a kernel may be off before its output's own rounding.
 
@@ -97,7 +98,9 @@ def attention(q, k, v, batch, n_rows, sm_scale, weight_ulp, v_step=None, sum_ulp
       sum_ulp |output|         where the weights' sum is of weights rounded by as
                                much: sum (p_t + e_t) v_t / sum (p_t + e_t) is off by
                                sum e_t (v_t - output), at most by |e_t v_t| and
-                               |e_t output| together."""
+                               |e_t output| together,
+      sum_least |output|       then also for each key, of a weight of 1: what a weight
+                               below the normal fp16 numbers is off by in the sum."""
     n_q = q.shape[1]
     heads, dh = k.shape[1], k.shape[3]
     out = np.full((n_rows, n_q, dh), np.nan)
@@ -118,5 +121,7 @@ def attention(q, k, v, batch, n_rows, sm_scale, weight_ulp, v_step=None, sum_ulp
                 out[m, g] = p @ vv / total
                 d = (dh + 8) * 2.0 ** -24 * (np.abs(qq) @ np.abs(kk).T * sm_scale).max(1, keepdims=True)
                 step = 2.0 ** -25 * np.abs(vv) if v_step is None else 2.0 ** -23 * v_step[pages, h, rows]
-                bound[m, g] = ((weight_ulp + 2 * d + 2.0 ** -21) * (p @ np.abs(vv)) + 2.0 ** -shift * step.sum(0)) / total + sum_ulp * np.abs(out[m, g])
+                bound[m, g] = ((weight_ulp + 2 * d + 2.0 ** -21) * (p @ np.abs(vv)) + 2.0 ** -shift * step.sum(0)) / total
+                if sum_ulp:
+                    bound[m, g] += (sum_ulp + sum_least * len(places) / total) * np.abs(out[m, g])
     return out, bound

@@ -39,6 +39,13 @@ constexpr int kPcK = 64;        // keys per tile
 // rescales in three of five tiles: 28/4 heads, four chunks of 512 over 8192 int8
 // tokens 378 us instead of 320.)
 constexpr float kChunkSlack = 3.f;
+// fp16 outputs over codes: the softmax's sum takes a key by its weight as rounded
+// to fp16, over the value's scale, so that a key that outweighs the others has
+// exactly its value.  A scale far below the unit brings that weight below the normal
+// numbers, or to 0, while the key's share of the sum stays what it is: keys whose
+// scale is less than kLeastShare units are summed by their exponentials.  (The
+// others' shares are off by 2^-11, or 2^-36 / kLeastShare of the largest weight.)
+constexpr float kLeastShare = 1.f / 256;
 
 template <int DH, int FMT, int NW>
 struct PcCfg {
@@ -49,7 +56,7 @@ struct PcCfg {
   static constexpr int kLoads = kPcK / RPI;                   // such loads of a tile's keys (or values)
   static constexpr int LPW = (kLoads + NW - 1) / NW;          // ... of a wave
   static constexpr int kTile = kPcK * DH * 2;
-  static constexpr int kScales = kInt ? 1024 : 0;             // key scales, value weights, their reciprocals, their unit
+  static constexpr int kScales = kInt ? 1024 : 0;             // key scales, value weights, their reciprocals (kLeastShare: 0), their unit, whether one is 0
   static constexpr int kBuf = 2 * kTile + kScales;
   static constexpr int OST = DH + 8;                          // halves of an output row in LDS
   static constexpr int kOut = NW * 32 * OST * 2;
@@ -302,9 +309,13 @@ paged_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws, int n_blk, 
         vref = value_unit(vref, wave_max(sane_scale(scale)));
         const float weight = scale * inverse_unit(vref);
         sc[64 + lane] = weight;
-        // (a weight of 0 or NaN, of a key that is not there or not seen, adds nothing)
-        if constexpr (kRoundedSum) sc[128 + lane] = weight > 0.f ? __builtin_amdgcn_rcpf(weight) : 0.f;
         if (lane == 0) sc[192] = vref;
+        if constexpr (kRoundedSum) {
+          const bool by_weight = weight >= kLeastShare;
+          sc[128 + lane] = by_weight ? __builtin_amdgcn_rcpf(weight) : 0.f;
+          const float any = __any(!by_weight) ? 1.f : 0.f;
+          if (lane == 0) sc[193] = any;
+        }
       }
     }
   };
@@ -473,6 +484,13 @@ paged_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws, int n_blk, 
           for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
             for (int v = 0; v < 16; ++v) ps[v & 3] += sacc[kk][v];
+        } else if (__builtin_amdgcn_readfirstlane(reinterpret_cast<const int*>(vb + C::kTile)[193])) {
+#pragma unroll
+          for (int q4 = 0; q4 < 8; ++q4) {
+            const f32x4 rs = *lds_at<f32x4>(saddr + 512 + 32 * q4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) ps[i] += rs[i] == 0.f ? sacc[q4 >> 2][4 * (q4 & 3) + i] : 0.f;
+          }
         }
         if (masked) {                                   // (the scale of a value that the query does not see may be NaN)
 #pragma unroll
@@ -505,9 +523,8 @@ paged_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws, int n_blk, 
           if constexpr (kBfMat) pf[e] = (__bf16)p;
           else pf[e] = (_Float16)p;
         }
-        // The weights' sum is taken of the weights as rounded, so that a key that
-        // outweighs the others has exactly its value.  (fp16 outputs; the sum of
-        // exponentials serves bf16 ones as well.)
+        // The weights' sum is taken of the weights as rounded (kLeastShare).  (The
+        // sum of exponentials serves bf16 outputs of codes as well.)
         if constexpr (!kInt) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) ps[e] = M::sum2(pf[2 * e], pf[2 * e + 1], ps[e]);
