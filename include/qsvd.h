@@ -510,7 +510,8 @@ qsvd_status qsvd_paged_read(const qsvd_pages* pages, const qsvd_page_batch* batc
  *   q, out    device [n_rows][ldq], [n_rows][ldo], n_q_heads heads of head_dim
  *   sm_scale  0 selects 1/sqrt(head_dim)
  *   ws        device workspace of at least the size query's bytes
- * A key or value row that is NaN or infinite reaches only queries that see it.
+ * A key or value row reaches only queries that see it, also one that is NaN,
+ * infinite or far larger than the others.
  * Calls that may overlap need workspaces of their own.  Lengths are read on the
  * device: a captured call may be replayed with other lengths up to max_len and
  * max_new.  A call repeats exactly for the same arguments; how a row's keys are

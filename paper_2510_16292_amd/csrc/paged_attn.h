@@ -134,6 +134,22 @@ __device__ __forceinline__ void direct_load4(const void* p, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(p) : "memory");
 }
 
+// Largest of the lanes up to each lane, and 0 (lane moves as above; rows of sixteen
+// lanes, then the first row's last lane to the second and the third's to the fourth,
+// then lane 31 to the upper half).
+__device__ __forceinline__ float max_upto(float x) {
+  auto move = [&](auto ctrl, auto rows) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), decltype(ctrl)::value, decltype(rows)::value, 0xf, true));
+  };
+  using All = std::integral_constant<int, 0xf>;
+  x = fmaxf(x, move(std::integral_constant<int, 0x111>(), All()));
+  x = fmaxf(x, move(std::integral_constant<int, 0x112>(), All()));
+  x = fmaxf(x, move(std::integral_constant<int, 0x114>(), All()));
+  x = fmaxf(x, move(std::integral_constant<int, 0x118>(), All()));
+  x = fmaxf(x, move(std::integral_constant<int, 0x142>(), std::integral_constant<int, 0xa>()));
+  return fmaxf(x, move(std::integral_constant<int, 0x143>(), std::integral_constant<int, 0xc>()));
+}
+
 constexpr int kMaxKeys = 1 << 30;     // of a sequence: a tile's end fits an int
 
 // A sequence of the step: its rows and what its queries may see.

@@ -14,7 +14,7 @@
 // the second product's operand being the first one's result in its lanes
 // (which keys a lane holds is the same for both), the values read transposed.
 // A key's scale multiplies its scores, a value's its weight, in units of a power
-// of two that bounds the value scales of the tiles so far.
+// of two that bounds the value scales of the keys that the query has seen so far.
 //
 // Long sequences with few rows are cut into parts along the keys, joined by
 // paged_join_chunk_kernel.
@@ -56,7 +56,9 @@ struct PcCfg {
   static constexpr int kLoads = kPcK / RPI;                   // such loads of a tile's keys (or values)
   static constexpr int LPW = (kLoads + NW - 1) / NW;          // ... of a wave
   static constexpr int kTile = kPcK * DH * 2;
-  static constexpr int kScales = kInt ? 1024 : 0;             // key scales, value weights, their reciprocals (kLeastShare: 0), their unit, whether one is 0
+  // Key scales, value weights, their reciprocals (kLeastShare: 0), value scales, the
+  // unit of those up to each key (the last: the tile's); whether a reciprocal is 0.
+  static constexpr int kScales = kInt ? 1536 : 0;
   static constexpr int kBuf = 2 * kTile + kScales;
   static constexpr int OST = DH + 8;                          // halves of an output row in LDS
   static constexpr int kOut = NW * 32 * OST * 2;
@@ -306,15 +308,17 @@ paged_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws, int n_blk, 
       float* sc = reinterpret_cast<float*>(vb + C::kTile);
       if (w == 0) sc[lane] = scale;
       if (w == 1) {
-        vref = value_unit(vref, wave_max(sane_scale(scale)));
+        const float upto = value_unit(vref, max_upto(sane_scale(scale)));
+        vref = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(upto), 63));
         const float weight = scale * inverse_unit(vref);
         sc[64 + lane] = weight;
-        if (lane == 0) sc[192] = vref;
+        sc[192 + lane] = scale;
+        sc[256 + lane] = upto;
         if constexpr (kRoundedSum) {
           const bool by_weight = weight >= kLeastShare;
           sc[128 + lane] = by_weight ? __builtin_amdgcn_rcpf(weight) : 0.f;
           const float any = __any(!by_weight) ? 1.f : 0.f;
-          if (lane == 0) sc[193] = any;
+          if (lane == 0) sc[320] = any;
         }
       }
     }
@@ -433,7 +437,11 @@ paged_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws, int n_blk, 
       // before the branch below: the compiler pads one side of it only.
       asm volatile("s_nop 7\n\ts_nop 7");
       __builtin_amdgcn_sched_barrier(0);
+      // tiles wholly before this wave's first query, inside the sequence and without holes need no mask
+      const bool masked = holes || !(kt0 + kPcK - 1 <= wave_first && kt0 + kPcK <= sq.kend);
+      const int lim = min(my_pos, sq.kend - 1) - kt0;   // the tile's last key that the query sees
       float vfac = 1.f;
+      float share = 1.f;                                // a query's unit over the tile's
       if constexpr (kInt) {
 #pragma unroll
         for (int q4 = 0; q4 < 8; ++q4) {
@@ -441,14 +449,17 @@ paged_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws, int n_blk, 
 #pragma unroll
           for (int i = 0; i < 4; ++i) sacc[q4 >> 2][4 * (q4 & 3) + i] *= ks[i];
         }
-        const float unit = reinterpret_cast<const float*>(vb + C::kTile)[192];
+        const float* units = reinterpret_cast<const float*>(vb + C::kTile) + 256;
+        float unit = units[63];
+        if (masked) {                                   // (a query's unit is of keys that it sees)
+          const float mine = lim < 0 ? o_unit : units[max(min(lim, 63), 0)];
+          share = mine * inverse_unit(unit);
+          unit = mine;
+        }
         vfac = o_unit * inverse_unit(unit);
         o_unit = unit;
       }
-      // tiles wholly before this wave's first query, inside the sequence and without holes need no mask
-      const bool masked = holes || !(kt0 + kPcK - 1 <= wave_first && kt0 + kPcK <= sq.kend);
       if (masked) {
-        const int lim = min(my_pos, sq.kend - 1) - kt0;
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
@@ -463,7 +474,7 @@ paged_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws, int n_blk, 
         mx = __builtin_elementwise_maximum(mx, __builtin_elementwise_maximum(sacc[0][v], sacc[1][v]));
       const float m_new = fa_pair_max(mx) * cs;
       const bool raise = m_new > m_run + kChunkSlack;   // (a row's own: others do not change its bits)
-      if (__any(raise) || vfac != 1.f) {
+      if (__any(raise || vfac != 1.f)) {
         const float alpha = raise ? __builtin_amdgcn_exp2f(m_run - m_new) : 1.f;
         m_run = raise ? m_new : m_run;
         l_run *= alpha;
@@ -484,22 +495,23 @@ paged_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws, int n_blk, 
           for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
             for (int v = 0; v < 16; ++v) ps[v & 3] += sacc[kk][v];
-        } else if (__builtin_amdgcn_readfirstlane(reinterpret_cast<const int*>(vb + C::kTile)[193])) {
+        } else if (__builtin_amdgcn_readfirstlane(reinterpret_cast<const int*>(vb + C::kTile)[320])) {
 #pragma unroll
           for (int q4 = 0; q4 < 8; ++q4) {
             const f32x4 rs = *lds_at<f32x4>(saddr + 512 + 32 * q4);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) ps[i] += rs[i] == 0.f ? sacc[q4 >> 2][4 * (q4 & 3) + i] : 0.f;
+            for (int i = 0; i < 4; ++i) l_run += rs[i] == 0.f ? sacc[q4 >> 2][4 * (q4 & 3) + i] : 0.f;
           }
         }
         if (masked) {                                   // (the scale of a value that the query does not see may be NaN)
+          const float inv_unit = inverse_unit(o_unit);
 #pragma unroll
           for (int q4 = 0; q4 < 8; ++q4) {
-            const f32x4 vs = *lds_at<f32x4>(saddr + 256 + 32 * q4);
+            const f32x4 vs = *lds_at<f32x4>(saddr + 768 + 32 * q4);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const int kk = q4 >> 2, v = 4 * (q4 & 3) + i;
-              sacc[kk][v] = 8 * q4 + 4 * hl + i <= min(my_pos, sq.kend - 1) - kt0 ? sacc[kk][v] * vs[i] : 0.f;
+              sacc[kk][v] = 8 * q4 + 4 * hl + i <= lim ? sacc[kk][v] * (vs[i] * inv_unit) : 0.f;
             }
           }
         } else {
@@ -542,7 +554,7 @@ paged_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws, int n_blk, 
         for (int ob = 0; ob < OB; ++ob) o[ob] = M::mfma32(vf[st & 1][ob], pf, o[ob]);
         __builtin_amdgcn_sched_barrier(0);
       }
-      l_run += (ps[0] + ps[1]) + (ps[2] + ps[3]);
+      l_run += kRoundedSum ? ((ps[0] + ps[1]) + (ps[2] + ps[3])) * share : (ps[0] + ps[1]) + (ps[2] + ps[3]);
       if constexpr (!kInt) {
         // values that are not finite (0 in the product), for the queries that see them
         if (odd) {

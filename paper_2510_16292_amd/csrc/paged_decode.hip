@@ -15,8 +15,8 @@
 // scores are eight consecutive keys, which is the operand layout of the second
 // product; the values come transposed out of LDS (ds_read_tr).  Codes are
 // widened to fp16, exactly; a key's scale multiplies its scores, a value's its
-// weight (in units of a power of two that bounds the value scales so far, which
-// keeps weights within fp16's normal numbers).
+// weight (in units of a power of two that bounds the value scales that the query
+// has seen so far, which keeps weights within fp16's normal numbers).
 //
 // What bounds it: the bytes of the cache.  32 heads of 128, 16 x 4096 16-bit
 // tokens: 1.07 GB in 187 us, 5.7 TB/s (a streaming read: 5.86); 28/4 heads, 32
@@ -235,11 +235,12 @@ paged_decode_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
   const int first_pos = sq.len - sq.n_new;              // of the first query: keys up to it need no causal mask
 
   f32x4 o[NQ][OB];
-  float m_run[NQ], l_run[NQ], vref = kLeastUnit;
+  float m_run[NQ], l_run[NQ], vref[NQ];
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
     m_run[n] = -INFINITY;
     l_run[n] = 0.f;
+    vref[n] = kLeastUnit;
 #pragma unroll
     for (int ob = 0; ob < OB; ++ob) o[n][ob] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
@@ -331,14 +332,13 @@ paged_decode_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) sc[n][e >> 2][e & 3] = e < lim ? sc[n][e >> 2][e & 3] : -INFINITY;
       }
-      if constexpr (kInt) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) vs[e] = e < hole_lim - 8 * g ? vs[e] : 0.f;
-      }
     }
-    float rs = 1.f, vfac = 1.f;
+    // Value scales in units of those that each query sees (as bits, which order
+    // alike; what is not finite is above the rest).
+    float rs[NQ], vfac[NQ];
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) rs[n] = vfac[n] = 1.f;
     if constexpr (kInt) {
-      // (as bits, which order alike; what is not finite is above the rest)
       uint32_t vb = 0;
 #pragma unroll
       for (int e = 0; e < 8; ++e) vb = max(vb, __float_as_uint(vs[e]));
@@ -348,12 +348,27 @@ paged_decode_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) vm = fmaxf(vm, sane_scale(vs[e]));
       }
-      const float last = vref;
-      vref = value_unit(vref, fa_rows4_max(vm));
-      rs = inverse_unit(vref);
-      vfac = last * rs;
+      vm = fa_rows4_max(vm);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) vs[e] *= rs;
+      for (int n = 0; n < NQ; ++n) {
+        float top = vm;
+        if (masked) {
+          const int lim = min(hole_lim, qpos[n] + 1 - k0) - 8 * g;
+          top = 0.f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) top = e < lim ? fmaxf(top, sane_scale(vs[e])) : top;
+          top = fa_rows4_max(top);
+        }
+        const float last = vref[n];
+        vref[n] = value_unit(last, top);
+        rs[n] = inverse_unit(vref[n]);
+        vfac[n] = last * rs[n];
+      }
+      if constexpr (NQ == 1) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) vs[e] *= rs[0];
+        rs[0] = 1.f;
+      }
     }
     X8 pf[NQ];
 #pragma unroll
@@ -365,19 +380,19 @@ paged_decode_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
       mx = fa_rows4_max(mx);
       const float m_new = mx * cs[n];
       const bool raise = m_new > m_run[n] + kSlack<BF, kInt>;   // (a row's own: others do not change its bits)
-      if (__any(raise) || vfac != 1.f) {
+      if (__any(raise || vfac[n] != 1.f)) {
         float ref = m_new;
         if constexpr (kInt && !BF) {
           // so that the weight of the largest score, its value's scale included, is a power of two
           float top = 0.f;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) top = sc[n][e >> 2][e & 3] == mx ? fmaxf(top, vs[e]) : top;
+          for (int e = 0; e < 8; ++e) top = sc[n][e >> 2][e & 3] == mx ? fmaxf(top, vs[e] * rs[n]) : top;
           ref += log2_mantissa(fa_rows4_max(top));
         }
         const float alpha = raise ? __builtin_amdgcn_exp2f(m_run[n] - ref) : 1.f;
         m_run[n] = raise ? ref : m_run[n];
         l_run[n] *= alpha;
-        const float ao = alpha * vfac;
+        const float ao = alpha * vfac[n];
 #pragma unroll
         for (int ob = 0; ob < OB; ++ob) o[n][ob] *= ao;
       }
@@ -391,9 +406,7 @@ paged_decode_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
       l_run[n] += sum;
       if constexpr (kInt) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          p[e] *= vs[e];
-        }
+        for (int e = 0; e < 8; ++e) p[e] *= vs[e] * rs[n];
         if (masked) {             // (a scale that is not finite, of a row that the query does not see)
           const int lim = min(hole_lim, qpos[n] + 1 - k0) - 8 * g;
 #pragma unroll
@@ -520,7 +533,7 @@ paged_decode_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
       }
     }
     float* stat = mine + 16 * C::kJoinRow;
-    if (g == 0) stat[r16] = m_run[n], stat[16 + r16] = l_run[n], stat[32 + r16] = kInt ? vref : 1.f;
+    if (g == 0) stat[r16] = m_run[n], stat[16 + r16] = l_run[n], stat[32 + r16] = kInt ? vref[n] : 1.f;
     __syncthreads();
     const int row = tid >> 4, ch = (tid & 15) * CT;
     float m = -INFINITY, mw[kPdWaves], l = 0.f, f[CT] = {};

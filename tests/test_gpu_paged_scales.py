@@ -77,3 +77,34 @@ def test_key_of_most_weight_with_no_value(fmt, dt, new, scale):
     # scores of key 7 about 5, of the others about 0: half to nearly all of the sum
     q = 0.6 + 0.1 * rng.standard_normal((new, 2 * dh))
     compare(p, 2, q=q)
+
+
+@pytest.mark.parametrize("fmt", [I8, I4], ids=["i8", "i4"])
+@pytest.mark.parametrize("dt", [HALF, BF], ids=["f16", "bf16"])
+@pytest.mark.parametrize("hq", [2, 14])
+@pytest.mark.parametrize("new,dh", [(5, 64), (12, 128), (100, 64), (200, 128)])
+def test_far_larger_value_reaches_only_who_sees_it(fmt, dt, hq, new, dh):
+    """A finite value row far larger than the others: queries before it are as if it were not there (bit for bit
+    but where the weights' sum is taken by what is large in a tile), those from it on within their bound."""
+    n = 230
+    p = Pool(fmt, dt, 2, dh, 16, [n], [new]).fill()
+    at = n - new // 2 - 1
+    pg, r = p.o.place(0, at)
+    q = to16(np.random.default_rng(3).standard_normal((new, hq * dh)), dt)
+    clean = values(p.attend(q, hq))
+    before, before_bound = p.want(q, hq)
+    rows = np.arange(n - new, n)
+    for scale in (2.0 ** 9,) if dt == HALF else (2.0 ** 9, 2.0 ** 40, 2.0 ** 100):
+        p.d.v_scale[pg, 1, r] = scale
+        got = values(p.attend(q, hq))
+        want, bound = p.want(q, hq)
+        head = (np.arange(hq * dh) // dh) // (hq // 2) == 1
+        assert_close(got[rows < at], before[rows < at], before_bound[rows < at], scale)
+        if p.sum_step(hq) == 0:
+            assert np.array_equal(got[rows < at], clean[rows < at]), scale
+        assert np.array_equal(got[:, ~head], clean[:, ~head]), scale
+        sees = rows >= at
+        with np.errstate(over="ignore"):
+            large = np.abs(want) > (65504 if dt == HALF else 3.38e38)
+        ok = sees[:, None] & ~large
+        assert_close(np.where(ok, got, 0), np.where(ok, want, 0), bound, scale)
