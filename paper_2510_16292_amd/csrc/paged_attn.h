@@ -121,6 +121,18 @@ __device__ __forceinline__ float value_unit(float unit, float top) {
 }
 __device__ __forceinline__ float inverse_unit(float unit) { return __uint_as_float(0x7f000000u - __float_as_uint(unit)); }
 
+// bf16 queries as fp16: the power of two that brings a row's largest, amax, to
+// [2^14, 2^15).  `cs`, score -> exponent of two, takes it back and stays a normal
+// number (a masked score, -inf, times 0 is NaN): where it would not, of rows or
+// scales that are tiny, the power is smaller, and the elements that fp16 then loses
+// move no score by 2^-13.
+__device__ __forceinline__ float query_up(float amax, float& cs) {
+  const int least = -112 - ((int)(__float_as_uint(cs) >> 23) - 127);
+  const int ex = min(max((int)(__float_as_uint(amax) >> 23) - 127, max(least, -100)), 127);
+  cs *= __uint_as_float((uint32_t)(127 + ex - 14) << 23);
+  return __uint_as_float((uint32_t)(127 + 14 - ex) << 23);
+}
+
 // Direct loads into LDS, lane p's bytes to lds + (bytes a lane) p (`lds`
 // wave-uniform): flash.hip says why they are asm.  They complete in order; the
 // wave waits for them with vmcnt.

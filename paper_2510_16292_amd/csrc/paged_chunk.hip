@@ -176,7 +176,6 @@ paged_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws, int n_blk, 
       if (in) x[s] = *reinterpret_cast<const i32x4*>(qp + 16 * s);
     }
     if constexpr (kInt && BF) {
-      // bf16 queries as fp16: a power of two brings the row's largest to [2^14, 2^15)
       float amax = 0.f;
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
@@ -186,9 +185,7 @@ paged_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws, int n_blk, 
         for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(f[e]));
       }
       amax = fa_pair_max(amax);
-      const int ex = min(max((int)(__float_as_uint(amax) >> 23) - 127, -100), 127);
-      const float up = __uint_as_float((uint32_t)(127 + 14 - ex) << 23);
-      cs *= __uint_as_float((uint32_t)(127 + ex - 14) << 23);
+      const float up = query_up(amax, cs);
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
         float f[8];

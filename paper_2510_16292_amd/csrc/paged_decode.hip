@@ -207,7 +207,6 @@ paged_decode_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
   for (int n = 0; n < NQ; ++n) {
     cs[n] = a.sm_scale * kFaLog2e;
     if constexpr (kInt && BF) {
-      // bf16 queries as fp16: a power of two brings the row's largest to [2^14, 2^15)
       float f[KS][8], amax = 0.f;
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
@@ -216,9 +215,7 @@ paged_decode_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
         for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(f[s][e]));
       }
       amax = fa_rows4_max(amax);
-      const int ex = min(max((int)(__float_as_uint(amax) >> 23) - 127, -100), 127);
-      const float up = __uint_as_float((uint32_t)(127 + 14 - ex) << 23);
-      cs[n] *= __uint_as_float((uint32_t)(127 + ex - 14) << 23);
+      const float up = query_up(amax, cs[n]);
 #pragma unroll
       for (int s = 0; s < KS; ++s)
 #pragma unroll

@@ -3,8 +3,6 @@ element against the oracle in 64 bits and its bound."""
 import numpy as np
 import pytest
 
-import gpu_harness as H
-from paper_2510_16292_amd import binding as B
 from test_gpu_paged import BF, FMT, HALF, I4, I8, Pool, assert_close, to16, values
 
 pytestmark = pytest.mark.gpu
