@@ -97,7 +97,7 @@ paged_join_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws) {
     if (row >= plan.chunk_rows || b >= a.batch.batch) continue;
     const PageSeq sq = page_seq(a.batch, a.page_bits, b);
     if (sq.n_new > a.batch.max_new || sq.n_new * G <= plan.few) continue;
-    const int parts = chunk_parts(plan, (max(sq.kend, 0) + 63) / 64, cut);
+    const int parts = chunk_parts(plan, chunk_tiles(sq.kend), cut);
     if (parts == 1) continue;
     float mx = -INFINITY, l = 0.f, y[8] = {};
     for (int p = 0; p < parts; ++p) mx = fmaxf(mx, ws.ml[p * plan.chunk_rows + row].x);
@@ -148,53 +148,13 @@ static hipError_t launch_attn(const PagedAttnArgs& a, const PagedPlan& p, const 
   return hipSuccess;
 }
 
-static PagedPlan paged_plan(const qsvd_pages& p, const qsvd_page_batch& b, int32_t n_q_heads) {
-  PagedPlan o{};
-  const int64_t groups = (int64_t)b.batch * p.n_kv_heads, rows = (int64_t)b.max_new * (n_q_heads / p.n_kv_heads);
-  // Sequences of up to 32 rows are the decode kernel's where all are; where some
-  // are longer, those of up to 16 rows, unless all bring the same.
-  if (rows <= 32) {
-    o.few = rows <= 16 ? 16 : 32;
-  } else {
-    o.chunk = true;
-    o.few = b.n_rows == (int64_t)b.batch * b.max_new ? 0 : 16;
-  }
-  const int64_t tiles = ((int64_t)b.max_len + kDecodeTile - 1) / kDecodeTile;
-  o.decode_slots = 256 * paged_decode_resident(p);
-  o.decode_parts = (int)std::max<int64_t>(1, std::min({o.decode_slots / groups, tiles / kDecodeMinTiles, (int64_t)128}));
-  o.decode_rows = groups * o.few;
-  if (o.few > 0 && b.batch > 1 && b.batch <= kChunkMaxBatch && tiles / o.decode_parts >= kDecodeCutTiles) {
-    o.decode_cut = true;
-    o.decode_parts = (int)std::min<int64_t>(tiles / kDecodeMinTiles, 128);
-    o.decode_rows = (o.decode_slots + groups) * o.few;  // (cut_by_lengths: at most so many workgroups)
-  }
-  o.few_rows = (int)std::min<int64_t>(o.few, rows);
-  o.chunk_parts = 1;
-  if (o.chunk) {
-    const int64_t seqs = std::max<int64_t>(1, std::min<int64_t>(b.batch, b.n_rows / b.max_new));   // about so many are long
-    const int64_t blocks = std::max<int64_t>(1, seqs * p.n_kv_heads * ((rows + 127) / 128));
-    const int64_t most = tiles / (2 * kChunkMinTiles);
-    if (b.batch > kChunkMaxBatch) {
-      // (every workgroup would look through all lengths)
-    } else if (2 * blocks <= kChunkSlots) {
-      o.chunk_parts = (int)std::max<int64_t>(1, std::min({kChunkSlots / blocks, most, (int64_t)16}));
-    } else if (blocks < 2 * kChunkSlots && tiles >= 128) {
-      o.cut = true;
-      o.chunk_parts = (int)std::min<int64_t>((2 * kChunkSlots - 1) / blocks + 1, most);
-    }
-  }
-  // (rows that a sequence has are below batch * max_new; more rows than that are spare)
-  o.chunk_rows = std::min(b.n_rows, (int64_t)b.batch * b.max_new) * n_q_heads;
-  return o;
-}
-
 size_t paged_attention_workspace(const qsvd_pages& p, const qsvd_page_batch& b, int32_t n_q_heads) {
-  return (size_t)paged_plan(p, b, n_q_heads).rows() * (p.head_dim * sizeof(float) + sizeof(float2));
+  return (size_t)paged_plan(b, p.n_kv_heads, n_q_heads, paged_decode_resident(p)).rows() * (p.head_dim * sizeof(float) + sizeof(float2));
 }
 
 hipError_t launch_paged_attention(const PagedAttnArgs& a, void* ws, hipStream_t s) {
   if (a.batch.n_rows == 0 || a.batch.max_new == 0) return hipSuccess;
-  const PagedPlan p = paged_plan(a.pages, a.batch, a.n_q_heads);
+  const PagedPlan p = paged_plan(a.batch, a.pages.n_kv_heads, a.n_q_heads, paged_decode_resident(a.pages));
   const PagedPartial part{(float*)ws, (float2*)((float*)ws + p.rows() * a.pages.head_dim)};
   const bool bf = a.pages.dtype == QSVD_BF16;
   if (a.pages.head_dim == 128) return bf ? launch_attn<true, 128>(a, p, part, s) : launch_attn<false, 128>(a, p, part, s);

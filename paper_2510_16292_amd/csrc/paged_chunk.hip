@@ -26,14 +26,10 @@
 // 247 us, int8 307 us, 720 TFLOP/s (a large product: 1200), the vector units busy
 // 0.46 of the time, the matrix cores 0.28: codes are widened and scales multiplied
 // besides, and 224 workgroups of 256 rows leave 32 CUs without.
-#include <algorithm>
-
 #include "paged_attn.h"
-#include "flash_map.h"
 
 namespace qsvd {
 
-constexpr int kPcK = 64;        // keys per tile
 // The softmax's reference is the largest score so far to within 2^kChunkSlack:
 // while no score exceeds it by more, nothing is rescaled.  (Without slack a wave
 // rescales in three of five tiles: 28/4 heads, four chunks of 512 over 8192 int8
@@ -93,52 +89,9 @@ paged_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws, int n_blk, 
   const int G = a.n_q_heads / a.pages.n_kv_heads;
   ChunkCut cut{};
   if (plan.cut) cut = chunk_cut(a.batch, plan, a.page_bits, a.pages.n_kv_heads, G, lane);
-  int grp, part, blk;
-  if (spread > 0) {
-    // A head's workgroups on one XCD (flash_map.h), which share its tiles there, the
-    // longest of all heads first; the first parts of all before the second (those
-    // past a sequence's number end at once).
-    const int groups = a.batch.batch * a.pages.n_kv_heads, each = gridDim.x / plan.chunk_parts;
-    part = blockIdx.x / each;
-    const FaWork work = fa_work(blockIdx.x - part * each, groups, n_blk, spread);
-    if (!work.any) return;
-    grp = work.group, blk = work.wg;
-  } else {
-    // Where sequences bring more or less (launch_chunk), the workgroups with work
-    // are counted off sequence by sequence, so that none is launched for the
-    // others and every XCD gets as many.
-    int left = blockIdx.x;
-    grp = -1;
-    for (int b0 = 0; b0 < a.batch.batch && grp < 0; b0 += 64) {
-      int items = 0, n_parts = 1;
-      if (b0 + lane < a.batch.batch) {
-        const PageSeq s = page_seq(a.batch, a.page_bits, b0 + lane);
-        if (s.n_new > 0 && s.n_new <= a.batch.max_new && s.n_new * G > plan.few) {
-          n_parts = chunk_parts(plan, (max(s.kend, 0) + kPcK - 1) / kPcK, cut);
-          items = a.pages.n_kv_heads * ((s.n_new * G + NW * 32 - 1) / (NW * 32)) * n_parts;
-        }
-      }
-      int upto = items;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const int x = __shfl_up(upto, o, 64);
-        upto += lane >= o ? x : 0;
-      }
-      const uint64_t mine = __ballot(upto > left);
-      if (mine) {
-        const int l = __builtin_ctzll(mine);
-        left -= __builtin_amdgcn_readlane(upto - items, l);
-        const int heads = a.pages.n_kv_heads, np = __builtin_amdgcn_readlane(n_parts, l);
-        const int blks = __builtin_amdgcn_readlane(items, l) / (heads * np);
-        grp = (b0 + l) * heads + left % heads;
-        part = left / heads % np;
-        blk = blks - 1 - left / (heads * np);
-      } else {
-        left -= __builtin_amdgcn_readlane(upto, 63);
-      }
-    }
-    if (grp < 0) return;
-  }
+  const ChunkWork work = chunk_work(a.batch, plan, cut, a.page_bits, a.pages.n_kv_heads, G, NW * 32, n_blk, spread, lane, blockIdx.x, gridDim.x);
+  const int grp = work.grp, part = work.part, blk = work.blk;
+  if (grp < 0) return;
   const int b = grp / a.pages.n_kv_heads, hk = grp - b * a.pages.n_kv_heads;
   const PageSeq sq = page_seq(a.batch, a.page_bits, b);
   if (sq.n_new <= 0 || sq.n_new > a.batch.max_new || sq.n_new * G <= plan.few) return;
@@ -147,7 +100,7 @@ paged_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws, int n_blk, 
   if (wg_r0 >= n_rows) return;
   int n_parts = 1;
   if (plan.chunk_parts > 1) {
-    n_parts = chunk_parts(plan, (max(sq.kend, 0) + kPcK - 1) / kPcK, cut);
+    n_parts = chunk_parts(plan, chunk_tiles(sq.kend), cut);
     n_parts = __builtin_amdgcn_readfirstlane(n_parts);
     if (part >= n_parts) return;
   }
@@ -650,23 +603,9 @@ static hipError_t launch_chunk(const PagedAttnArgs& a, const PagedPlan& p, const
   constexpr int lds = PcCfg<DH, FMT, NW>::kLds;
   const hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   if (e != hipSuccess) return e;
-  const int64_t rows = (int64_t)a.batch.max_new * (a.n_q_heads / a.pages.n_kv_heads);
-  const int n_blk = (int)((rows + NW * 32 - 1) / (NW * 32));
-  const int64_t groups = (int64_t)a.batch.batch * a.pages.n_kv_heads;
-  int spread = fa_parts(groups, n_blk);
-  int64_t blocks = fa_blocks(groups, n_blk, spread) * p.chunk_parts;
-  if ((p.few > 0 || p.cut) && a.batch.batch <= kChunkMaxBatch) {
-    // As many workgroups as there can be work for: whole blocks of the step's rows
-    // and one more per sequence, times their parts; where the parts follow from the
-    // lengths, kChunkSlots more (chunk_cut: at most so many, or half of them and
-    // one for each block).
-    spread = 0;
-    const int64_t n = std::min(a.batch.n_rows, (int64_t)a.batch.batch * a.batch.max_new), G = a.n_q_heads / a.pages.n_kv_heads;
-    blocks = a.pages.n_kv_heads * (n * G / (NW * 32) + std::min<int64_t>(a.batch.batch, n));
-    blocks = p.cut ? blocks + kChunkSlots : blocks * p.chunk_parts;
-  }
+  const ChunkGrid g = chunk_grid(a.batch, p, a.pages.n_kv_heads, a.n_q_heads / a.pages.n_kv_heads, NW);
   KernelScope ks("paged_chunk", s);
-  QSVD_LAUNCH(ks, kern, dim3((unsigned)blocks), dim3(NW * 64), lds, s, a, p, ws, n_blk, spread);
+  QSVD_LAUNCH(ks, kern, dim3((unsigned)g.blocks), dim3(NW * 64), lds, s, a, p, ws, g.n_blk, g.spread);
   return hipGetLastError();
 }
 
