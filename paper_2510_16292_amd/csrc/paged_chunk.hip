@@ -95,7 +95,7 @@ paged_chunk_kernel(PagedAttnArgs a, PagedPlan plan, PagedPartial ws, int n_blk, 
   const int b = grp / a.pages.n_kv_heads, hk = grp - b * a.pages.n_kv_heads;
   const PageSeq sq = page_seq(a.batch, a.page_bits, b);
   if (sq.n_new <= 0 || sq.n_new > a.batch.max_new || sq.n_new * G <= plan.few) return;
-  const int n_rows = sq.n_new * G;
+  const int n_rows = sq.rows * G;
   const int wg_r0 = blk * NW * 32;
   if (wg_r0 >= n_rows) return;
   int n_parts = 1;

@@ -20,6 +20,7 @@ constexpr int kMaxKeys = 1 << 30;     // of a sequence: a tile's end fits an int
 struct PageSeq {
   int n_new;        // new tokens; 0: none
   int row0;         // first row
+  int rows;         // rows: new tokens, but none at or past n_rows
   int len;          // tokens, the new ones included
   int kend;         // keys: len, but at most what the table has places for
 };
@@ -27,6 +28,7 @@ __device__ __forceinline__ PageSeq page_seq(const qsvd_page_batch& t, int page_b
   PageSeq s;
   s.row0 = t.first[b];
   s.n_new = t.first[b + 1] - s.row0;
+  s.rows = (int)max((int64_t)0, min((int64_t)s.n_new, t.n_rows - s.row0));
   s.len = t.seq_len[b];
   s.kend = (int)min((int64_t)min(s.len, kMaxKeys), (int64_t)t.max_pages << page_bits);
   return s;
@@ -131,7 +133,7 @@ __device__ __forceinline__ ChunkCut chunk_cut(const qsvd_page_batch& t, const Pa
       [&](int b) {
         const PageSeq s = page_seq(t, page_bits, b);
         if (s.n_new <= 0 || s.n_new > t.max_new || s.n_new * G <= p.few) return make_int2(0, 0);
-        return make_int2((s.n_new * G + 127) / 128, chunk_tiles(s.kend));
+        return make_int2((s.rows * G + 127) / 128, chunk_tiles(s.kend));
       },
       [&](int tiles, const ChunkCut& c) { return chunk_parts(p, tiles, c); });
 }
@@ -190,7 +192,7 @@ __device__ __forceinline__ ChunkWork chunk_work(const qsvd_page_batch& t, const 
       const PageSeq s = page_seq(t, page_bits, b0 + lane);
       if (s.n_new > 0 && s.n_new <= t.max_new && s.n_new * G > p.few) {
         n_parts = chunk_parts(p, chunk_tiles(s.kend), cut);
-        items = n_kv_heads * ((s.n_new * G + rows - 1) / rows) * n_parts;
+        items = n_kv_heads * ((s.rows * G + rows - 1) / rows) * n_parts;
       }
     }
     int upto = items;

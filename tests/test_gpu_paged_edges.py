@@ -3,7 +3,7 @@ oracle in 64 bits and its bound."""
 import numpy as np
 import pytest
 
-from test_gpu_paged import BF, FORM_IDS, FORMS, Pool, assert_close, to16, values
+from test_gpu_paged import BF, F16, FORM_IDS, FORMS, HALF, I4, I8, Pool, assert_close, bits, to16, values
 
 pytestmark = pytest.mark.gpu
 
@@ -21,3 +21,41 @@ def test_queries_of_zeros_and_tiny_ones(fmt, dt, new, scale):
     got = values(p.attend(d, 4, scale))
     want, bound = p.want(d, 4, scale)
     assert_close(got, want, bound, scale)
+
+
+@pytest.mark.parametrize("fmt,dt", FORMS, ids=FORM_IDS)
+@pytest.mark.parametrize("heads,hq,lens,news,n_rows", [
+    (1, 1, [50, 900], [50, 900], 100), (1, 1, [40, 300, 300], [40, 300, 300], 400), (1, 1, [1000], [1000], 100),
+    (2, 4, [300, 1500, 70], [1, 200, 70], 60), (1, 4, [2000, 90], [300, 1], 299), (4, 4, [20, 400, 30], [20, 130, 1], 150),
+    (1, 1, [64, 64, 500], [64, 64, 500], 128), (2, 4, [70, 80, 90], [5, 3, 4], 6), (1, 2, [300], [300], 1),
+])
+def test_rows_that_are_not_there_any_more(fmt, dt, heads, hq, lens, news, n_rows):
+    """n_rows below the step's rows, also inside a chunk: the rows before it are as ever, the others left alone."""
+    dh, n = 64, sum(news)
+    p = Pool(fmt, dt, heads, dh, 16, lens, news).fill()
+    q = to16(np.random.default_rng(0).standard_normal((n, hq * dh)), dt)
+    q[n_rows:] = float("nan")
+    p.rebatch(lens, news, n_rows=n_rows)
+    got = values(p.attend(q, hq))
+    want, bound = p.want(q[:n_rows], hq)
+    assert (got[n_rows:] == 3.0).all()
+    assert_close(got[:n_rows], want, bound)
+
+
+@pytest.mark.parametrize("fmt", [F16, I8, I4], ids=["f16", "i8", "i4"])
+def test_append_and_read_of_rows_that_are_there(fmt):
+    """n_rows inside a sequence's rows: the tokens behind it are neither written nor read."""
+    lens, news, n_rows = [40, 50], [40, 45], 60
+    p = Pool(fmt, HALF, 2, 64, 16, lens, news)
+    rows = to16(np.random.default_rng(1).standard_normal((85, 128)), HALF)
+    p.rebatch(lens, news, n_rows=n_rows)
+    before = bits(p.d.k)
+    p.append(rows, rows)
+    places = [p.o.place(b, pos) for _, b, pos in p.o.rows(n_rows)]
+    changed = (bits(p.d.k) != before).reshape(p.n_pages, 2, p.page, -1).any((1, 3))
+    assert sorted(zip(*np.nonzero(changed))) == sorted(places) and len(places) == n_rows
+    back = [rows.clone().fill_(6.0) for _ in range(2)]
+    p.read(*back)
+    got = values(back[0])
+    assert (got[n_rows:] == 6.0).all() and np.array_equal(got, values(back[1]))
+    assert np.abs(got[:n_rows] - values(rows)[:n_rows]).max() <= {F16: 0, I8: 0.02, I4: 0.4}[fmt]

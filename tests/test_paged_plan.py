@@ -246,6 +246,8 @@ def program(tmp_path_factory):
     return str(exe)
 
 
-def test_every_block_and_part_once(program):
-    res = subprocess.run([program, "90", "0"], capture_output=True, text=True, timeout=110)
+@pytest.mark.parametrize("inside", ["0", "1"], ids=["all", "n_rows-inside"])
+def test_every_block_and_part_once(program, inside):
+    """inside: n_rows is below the step's rows, whose last ones have no place in Q and the outputs."""
+    res = subprocess.run([program, "90", inside], capture_output=True, text=True, timeout=110)
     assert res.returncode == 0, res.stdout
