@@ -3,7 +3,7 @@ element against the oracle in 64 bits and its bound."""
 import numpy as np
 import pytest
 
-from test_gpu_paged import BF, FMT, HALF, I4, I8, Pool, assert_close, to16, values
+from test_gpu_paged import BF, F16, FMT, HALF, I4, I8, Pool, assert_close, to16, values
 
 pytestmark = pytest.mark.gpu
 
@@ -106,3 +106,37 @@ def test_far_larger_value_reaches_only_who_sees_it(fmt, dt, hq, new, dh):
             large = np.abs(want) > (65504 if dt == HALF else 3.38e38)
         ok = sees[:, None] & ~large
         assert_close(np.where(ok, got, 0), np.where(ok, want, 0), bound, scale)
+
+
+@pytest.mark.parametrize("fmt", [F16, I8, I4], ids=["f16", "i8", "i4"])
+@pytest.mark.parametrize("dt", [HALF, BF], ids=["f16", "bf16"])
+@pytest.mark.parametrize("new", [1, 20, 90])
+@pytest.mark.parametrize("down", [12.0, 24.7, 25.5, 28.3, 31.0])
+def test_keys_of_small_weight_beside_one_of_most(fmt, dt, new, down):
+    """A key whose value is 0 holds nearly all of the softmax; the others, 2^-down of it each, are the output."""
+    rng = np.random.default_rng(6)
+    n, dh = 400, 64
+    p = Pool(fmt, dt, 1, dh, 16, [n], [new])
+    keys = np.zeros((n, 1, dh))
+    vals = 1000 * rng.uniform(0.5, 1, (n, 1, dh))
+    keys[3], vals[3] = 1.0, 0.0
+    fill_values(p, keys, vals)
+    q = np.full((new, 2 * dh), down * np.log(2) / 8)                # score of key 3: 64 q / 8, of the others 0
+    got = compare(p, 2, q=q)
+    assert (got > 0).all()
+
+
+@pytest.mark.parametrize("fmt", [F16, I8, I4], ids=["f16", "i8", "i4"])
+@pytest.mark.parametrize("dt", [HALF, BF], ids=["f16", "bf16"])
+@pytest.mark.parametrize("new", [1, 40])
+def test_many_keys_of_small_weight_keep_their_share_of_the_sum(fmt, dt, new):
+    """2^18 keys of weight 2^-25.5 beside one of weight 1, together 1.0055, all values 1: the outputs are 1, off by
+    three roundings (weights, their sum, the output)."""
+    n, dh = 1 << 18, 64
+    p = Pool(fmt, dt, 1, dh, 64, [n], [new], poison=False)
+    keys = np.zeros((n, 1, dh))
+    keys[3] = 1.0
+    fill_values(p, keys, np.ones((n, 1, dh)))
+    q = to16(np.full((new, dh), 25.5 * np.log(2) / 8), dt)
+    got = values(p.attend(q, 1))
+    assert np.abs(got - 1).max() <= (3.01 * 2.0 ** -11 if dt == HALF else 3.01 * 2.0 ** -8)
