@@ -403,8 +403,9 @@ qsvd_status qsvd_linear_i8(const void* xq, int64_t ldx, const float* sx, const v
  * wider than its latent (2 * 4 heads of 128: r = 1024).  For such layers these
  * calls turn Q and K once, keep K and V of every token in pages (16-bit rows,
  * or int8 / int4 codes with a scale per token and head), and attend over the
- * pages.  A layer's step: qsvd_lowrank_qkv_prefill (Q, K, V), qsvd_rope_axes,
- * qsvd_paged_append, qsvd_paged_attention, qsvd_linear_i8.  `dtype`
+ * pages.  A layer's step: Q, K, V (qsvd_lowrank_qkv_prefill in fp16, or
+ * qsvd_linear_i8 in either type), qsvd_rope_axes, qsvd_paged_append,
+ * qsvd_paged_attention, qsvd_linear_i8.  `dtype`
  * (QSVD_F16 or QSVD_BF16) is the type of every 16-bit operand. */
 
 enum { QSVD_ROPE_MAX_AXES = 4 };
@@ -489,7 +490,8 @@ typedef struct {
  * head scale NaN and codes 0.  F16 rows are copied.
  *   k, v  device [n_rows][ldk], [n_rows][ldv], heads next to each other
  * Lengths and tables are not changed: the caller advances seq_len before the
- * step, once for all layers.  If two rows have the same place, either may stay.
+ * step, once for all layers.  If two rows of a step have the same place, it is
+ * left with a mixture of both (the codes of one, the scale of the other).
  * Requires n_kv_heads <= 256, n_rows and max_new < 2^22, batch <= 65536, max_len
  * <= 2^30, 16-byte aligned rows and pages, 0 < clip <= 1. */
 qsvd_status qsvd_paged_append(const qsvd_pages* pages, const qsvd_page_batch* batch, const void* k, int64_t ldk,
@@ -511,7 +513,13 @@ qsvd_status qsvd_paged_read(const qsvd_pages* pages, const qsvd_page_batch* batc
  *   sm_scale  0 selects 1/sqrt(head_dim)
  *   ws        device workspace of at least the size query's bytes
  * A key or value row reaches only queries that see it, also one that is NaN,
- * infinite or far larger than the others.
+ * infinite or far larger than the others (but for low-order bits of fp16 outputs
+ * over codes, where a value scale is 2^8 times larger).
+ * Weights are rounded to 16 bits before they meet the values: to bf16 over bf16
+ * rows, else to fp16, where a weight (over codes: times its value's scale, against
+ * the largest that the query sees) loses bits below 2^-25 of the row's largest and
+ * counts for nothing below 2^-36; the sum that they are divided by is off by no
+ * more.  Sums are fp32: bf16 values past 2^84 may overflow them.
  * Calls that may overlap need workspaces of their own.  Lengths are read on the
  * device: a captured call may be replayed with other lengths up to max_len and
  * max_new.  A call repeats exactly for the same arguments; how a row's keys are
