@@ -22,18 +22,19 @@
 // What bounds it: the vector operations of the softmax beside the products, which
 // hardly overlap (alone a wave's tile takes 0.47 us of products and 0.5 us of
 // vector operations, together 1.1).  28/4 heads of 128, one prompt of 8192 16-bit
-// tokens: 500 us, 960 TFLOP/s; four chunks of 512 over up to 8192 tokens: 16-bit
-// 247 us, int8 307 us, 720 TFLOP/s (a large product: 1200), the vector units busy
-// 0.46 of the time, the matrix cores 0.28: codes are widened and scales multiplied
-// besides, and 224 workgroups of 256 rows leave 32 CUs without.
+// tokens: 500 us, 960 TFLOP/s, the vector units busy 0.43 of the time, the matrix
+// cores 0.41; four chunks of 512 over up to 8192 tokens: 16-bit 251 us, int8 303 us,
+// 730 TFLOP/s (a large product: 1200), the vector units busy 0.46 of the time, the
+// matrix cores 0.29: codes are widened and scales multiplied besides, and 224
+// workgroups of 256 rows leave 32 CUs without.
 #include "paged_attn.h"
 
 namespace qsvd {
 
 // The softmax's reference is the largest score so far to within 2^kChunkSlack:
 // while no score exceeds it by more, nothing is rescaled.  (Without slack a wave
-// rescales in three of five tiles: 28/4 heads, four chunks of 512 over 8192 int8
-// tokens 378 us instead of 320.)
+// rescales in three of five tiles: 28/4 heads, four chunks of 512 over 8192 tokens
+// int8 307 us instead of 305, int4 311 instead of 307, 16 bits 254 instead of 251.)
 constexpr float kChunkSlack = 3.f;
 // fp16 outputs over codes: the softmax's sum takes a key by its weight as rounded
 // to fp16, over the value's scale, so that a key that outweighs the others has
@@ -611,10 +612,10 @@ static hipError_t launch_chunk(const PagedAttnArgs& a, const PagedPlan& p, const
 
 // Eight waves share the tiles' widening and LDS copies where there are rows for
 // several such workgroups, four (two workgroups per CU) otherwise: us, four and
-// eight waves, heads of 128: 28/4, four chunks of 512 over 8192 tokens int8 368,
-// 319, int4 378, 343, 16-bit 262, 250; one of 1024 over 16384 int8 381, 332; 32
-// heads, 4 x 640 tokens 16-bit 33.2, 41.2, int8 35.7, 45.2; 28/4, 16 x 8 over 4096
-// int8 38.5, 55.1.
+// eight waves, heads of 128: 28/4, four chunks of 512 over 8192 tokens int8 336,
+// 305, int4 350, 307, 16-bit 274, 251; one of 1024 over 16384 int8 340, 306; 32
+// heads, 4 x 640 tokens 16-bit 34.3, 40.1, int8 37.3, 47.4; 28/4, 16 x 8 over 4096
+// int8 37.9, 50.0.
 template <bool BF, int DH, int FMT>
 static hipError_t launch_chunk(const PagedAttnArgs& a, const PagedPlan& p, const PagedPartial& ws, hipStream_t s) {
   const int64_t rows = (int64_t)a.batch.max_new * (a.n_q_heads / a.pages.n_kv_heads);

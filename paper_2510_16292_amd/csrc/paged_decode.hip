@@ -21,10 +21,10 @@
 // What bounds it: the bytes of the cache.  32 heads of 128, 16 x 4096 16-bit
 // tokens: 1.07 GB in 187 us, 5.7 TB/s (a streaming read: 5.86); 28/4 heads, 32
 // sequences of up to 8192 int8 tokens: 247 MB in 50 us, 5.0 TB/s.  One sequence of
-// 30001 16-bit tokens of 4 heads, 61 MB, takes 14.6 us, a quarter of it the first
-// loads' latency and the last waves' join.  int4 codes are bound by their widening:
-// 40 heads, 8 sequences of up to 4096 tokens, 159 MB in 38 us, 4.2 TB/s, the vector
-// units busy 0.55 of the time.
+// 30001 16-bit tokens of 4 heads, 61 MB, takes 14.3 us, a quarter of it the first
+// loads' latency and the last waves' join.  With int4 codes no unit is the bound by
+// itself: 40 heads, 8 sequences of up to 4096 tokens, 159 MB in 39.5 us, 4.0 TB/s, the
+// vector units (more than half of whose operations widen codes) busy 0.55 of the time.
 #include <algorithm>
 
 #include "paged_attn.h"

@@ -53,11 +53,12 @@ constexpr int kDecodeTile = 32;       // keys of a wave's tile
 constexpr int kDecodeWaves = 4;
 constexpr int kDecodeMinTiles = 8;    // ... of a part
 // Where the longest sequence's workgroups may have so many tiles, their parts follow
-// from all lengths.  That costs 3 to 10 us and gains where few are long: us, as many
+// from all lengths.  That costs 3 to 20 us and gains where few are long: us, as many
 // parts for each and by all lengths, 28/4 heads of 128, one of 32768 tokens among 63
-// of 1000 in 16 bits 252, 51, in int4 78, 28; 64 of 32768 706, 717; 32 heads, one of
-// 16384 among 15 of 500 int8 177, 48; and with fewer tiles, 28/4 heads, 16
-// sequences of 400 to 8192 in 16 bits (128) 50, 54, 32 heads, 16 of 4096 190, 196.
+// of 1000 in 16 bits 251, 51, in int4 80, 28; 64 of 32768 705, 716; one of 8192 among
+// 255 of 300 in 16 bits 77, 99, int8 96, 84; 32 heads, one of 16384 among 15 of 500
+// int8 183, 49; and with fewer tiles, 28/4 heads, 16 sequences of 400 to 8192 in 16
+// bits (128) 50, 54, 32 heads, 16 of 4096 190, 196.
 constexpr int kDecodeCutTiles = 256;
 
 // The chunk kernel's parts.  Where there are workgroups for two or more parts of
@@ -69,7 +70,7 @@ constexpr int kDecodeCutTiles = 256;
 // that, at which the parts are no more than those workgroups (a part more would be
 // a second round), else twice that.  The calling wave's lanes count; all receive it.
 // us, without cutting and with: 28/4 heads of 128, 16 chunks of 100 tokens over
-// 820 to 8192 int4 381, 268, in a batch of 64 with 48 single tokens 390, 305.
+// 820 to 8192 int4 339, 241, in a batch of 64 with 48 single tokens 338, 288.
 constexpr int kChunkMinTiles = 8;
 constexpr int kChunkMaxBatch = 1024;
 constexpr int kChunkSlots = 512;      // workgroups of 128 rows that the chip holds
