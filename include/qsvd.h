@@ -448,7 +448,7 @@ qsvd_status qsvd_rope_axes(const qsvd_rope* rope, const int32_t* pos, int64_t ld
  * consecutive tokens of one sequence, every head's rows together:
  *   F16   k, v are [n_pages][n_kv_heads][page_size][head_dim] of dtype, scales NULL
  *   I8    ... int8 codes, I4 packed int4 codes ([head_dim / 2] bytes), and
- *         k_scale, v_scale are fp32 [n_pages][n_kv_heads][page_size] */
+ *         k_scale, v_scale are fp32 [n_pages][n_kv_heads][page_size], not negative */
 typedef struct {
   int32_t fmt;         /* QSVD_CACHE_*; F16 means rows of dtype */
   int32_t dtype;       /* type of K, V, Q and the outputs, and of F16 rows */

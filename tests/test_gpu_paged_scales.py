@@ -79,7 +79,7 @@ def test_key_of_most_weight_with_no_value(fmt, dt, new, scale):
 
 @pytest.mark.parametrize("fmt", [I8, I4], ids=["i8", "i4"])
 @pytest.mark.parametrize("dt", [HALF, BF], ids=["f16", "bf16"])
-@pytest.mark.parametrize("hq", [2, 14])
+@pytest.mark.parametrize("hq", [2, 8, 14])
 @pytest.mark.parametrize("new,dh", [(5, 64), (12, 128), (100, 64), (200, 128)])
 def test_far_larger_value_reaches_only_who_sees_it(fmt, dt, hq, new, dh):
     """A finite value row far larger than the others: queries before it are as if it were not there (bit for bit
