@@ -118,7 +118,7 @@ paged_rows_kernel(PagedRowsArgs a) {
   const bool live = row && b < a.batch.batch;
   int64_t at = -1;                                  // the row of head h0 in the pool; the next head's is a page further
   if (live) {
-    const int pos = a.batch.seq_len[b] - (int)(a.batch.first[b + 1] - m);
+    const int pos = max(a.batch.seq_len[b], -(1 << 30)) - (int)(a.batch.first[b + 1] - m);   // (negative stays so)
     const int page = page_of(a.batch, a.pages.n_pages, a.page_bits, b, pos);
     if (page >= 0)
       at = (((int64_t)page * a.pages.n_kv_heads + h0) << a.page_bits) + (pos & (a.pages.page_size - 1));

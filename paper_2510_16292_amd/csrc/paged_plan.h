@@ -29,7 +29,7 @@ __device__ __forceinline__ PageSeq page_seq(const qsvd_page_batch& t, int page_b
   s.row0 = t.first[b];
   s.n_new = t.first[b + 1] - s.row0;
   s.rows = (int)max((int64_t)0, min((int64_t)s.n_new, t.n_rows - s.row0));
-  s.len = t.seq_len[b];
+  s.len = max(t.seq_len[b], -kMaxKeys);               // (positions below it stay negative)
   s.kend = (int)min((int64_t)min(s.len, kMaxKeys), (int64_t)t.max_pages << page_bits);
   return s;
 }

@@ -59,3 +59,33 @@ def test_append_and_read_of_rows_that_are_there(fmt):
     got = values(back[0])
     assert (got[n_rows:] == 6.0).all() and np.array_equal(got, values(back[1]))
     assert np.abs(got[:n_rows] - values(rows)[:n_rows]).max() <= {F16: 0, I8: 0.02, I4: 0.4}[fmt]
+
+
+@pytest.mark.parametrize("fmt,dt", FORMS, ids=FORM_IDS)
+@pytest.mark.parametrize("news", [[1, 1, 1, 1], [3, 2, 4, 1], [40, 1, 60, 7]])
+def test_negative_lengths(fmt, dt, news):
+    """Sequences whose new tokens have negative positions, down to the type's lowest: not written, zeros read and
+    zeros as outputs; the sequence next to them is as ever."""
+    lens = [-(2 ** 31), 50, -1, -(2 ** 31) + 5]
+    n = sum(news)
+    p = Pool(fmt, dt, 2, 64, 16, lens, news)
+    p.table = np.where(p.table < 0, 1, p.table).astype(np.int32)        # every column names a page
+    p.rebatch([0, 50, 0, 0], [0, 50, 0, 0])
+    rows = to16(np.random.default_rng(0).standard_normal((50, 128)), dt)
+    p.append(rows, rows)
+    p.rebatch(lens, news, max_len=50)
+    before = bits(p.d.k)
+    new = to16(np.random.default_rng(1).standard_normal((n, 128)), dt)
+    mine = np.arange(news[0], news[0] + news[1])
+    new[mine] = rows[-news[1]:]                                           # the second sequence's as they are
+    p.append(new, new)
+    assert np.array_equal(bits(p.d.k), before)
+    back = [new.clone().fill_(6.0) for _ in range(2)]
+    p.read(*back)
+    others = np.setdiff1d(np.arange(n), mine)
+    assert not values(back[0])[others].any() and (values(back[1])[mine] != 0).any()
+    q = to16(np.random.default_rng(2).standard_normal((n, 4 * 64)), dt)
+    got = values(p.attend(q, 4))
+    want, bound = p.want(q, 4)
+    assert not want[others].any()
+    assert_close(got, want, bound)
